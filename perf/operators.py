@@ -1,0 +1,409 @@
+"""The policy's side of a training loop around the environments, as cases that can be timed and compared.
+
+Three operators, each on what a policy and a rollout hand over:
+
+  sample      one action a row from logits and given uniform numbers: a mask of what is allowed, a
+              temperature, top-k, top-p and min-p, and the log-probability of the action under the policy
+  advantages  generalised advantages and returns of a rollout, from its rewards and done flags and
+              the network's values, backwards over the steps of each environment
+  loss        the clipped policy loss with an entropy bonus and a value loss, and its gradients
+              with respect to the logits and the values
+
+A policy of the narrow representation has a logit for each tile type (2, 4 or 7 classes); one that also
+chooses the cell has one for each cell and tile type, up to 64 * 64 * 7.  Rows may be padded
+(a stride beyond the classes).  `run` computes them in plain torch operations, or, with `own`, through
+the framework's entry points.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DTYPES = {"float32": torch.float32, "bfloat16": torch.bfloat16, "float16": torch.float16}
+TILES = [2, 4, 7]
+MOST_CLASSES = 64 * 64 * 7
+MOST_LOGITS = 1024 * MOST_CLASSES      # a case's rows times classes
+MOST_STEPS = 32 * 262144               # steps times environments of advantages
+PAD = 8                                # elements behind a row, where rows are padded
+WEIGHTS = dict(clip_low=0.2, clip_high=0.2, entropy_coef=0.01, value_coef=0.5)
+
+
+def _sample(rows, classes, dtype, **more):
+    c = dict(kind="sample", rows=rows, classes=classes, dtype=dtype, masked=False, padded=False, temperature=1.0,
+             top_k=0, top_p=1.0, min_p=0.0)
+    c.update(more)
+    return c
+
+
+def _loss(rows, classes, dtype, **more):
+    c = dict(kind="loss", rows=rows, classes=classes, dtype=dtype, masked=False, padded=False, temperature=1.0,
+             values=True, clipped=True)
+    c.update(more)
+    return c
+
+
+def _advantages(steps, envs, dtype, **more):
+    c = dict(kind="advantages", steps=steps, envs=envs, dtype=dtype, discount=0.99, trace=0.95, episode=1000)
+    c.update(more)
+    return c
+
+
+def listed():
+    return [
+        # the smallest call: the next step of 64 levels waits for these actions
+        _sample(64, 2, "float32", name="sample_binary16_b64"),
+        # the usual training batch, seven tile types, exploration a little above the policy's own
+        _sample(16384, 7, "bfloat16", temperature=1.1, name="sample_dungeon32_b16384"),
+        # a cell and a tile of a 16x16 maze, in training: no truncation, cells outside the map masked
+        _sample(4096, 1024, "bfloat16", masked=True, name="sample_cells16_b4096"),
+        # one level in a designer's editor: a single row, the few best edits
+        _sample(1, 16384, "float32", masked=True, temperature=0.7, top_k=50, top_p=0.9, name="sample_cells64_b1"),
+        # diverse levels from a trained policy over a large map: the largest rows, every filter but top-k
+        _sample(1024, 28672, "bfloat16", masked=True, top_p=0.95, min_p=0.002, name="sample_cells64_b1024"),
+        # rollouts of 64 levels over 256 steps, values in the network's type
+        _advantages(256, 64, "float32", name="advantages_t256_b64"),
+        # a whole long run of a few levels: the time axis is what there is to share out
+        _advantages(10000, 16, "bfloat16", episode=300, name="advantages_t10000_b16"),
+        # the largest batch
+        _advantages(32, 262144, "bfloat16", name="advantages_t32_b262144"),
+        # a minibatch of small rollouts
+        _loss(16384, 2, "float32", name="loss_binary16_n16384"),
+        # an epoch's minibatch of large rollouts, seven tile types
+        _loss(2097152, 7, "bfloat16", name="loss_dungeon32_n2097152"),
+        # ragged rows of a 27x45 dungeon, padded, with the cells outside the map masked; no critic
+        _loss(1001, 8505, "float16", masked=True, padded=True, values=False, name="loss_cells27x45_n1001"),
+        # a cell and a tile of a 64x64 maze
+        _loss(1024, 16384, "bfloat16", masked=True, name="loss_cells64_n1024"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choices(["sample", "loss", "advantages"], [45, 30, 25])[0]
+    dtype = rng.choice(sorted(DTYPES))
+    if kind == "advantages":
+        steps = _log_int(rng, 1, 10000)
+        envs = _log_int(rng, 1, max(1, MOST_STEPS // max(steps, 32)))
+        return _advantages(steps, envs, dtype, discount=rng.choice([0.99, 0.9, 1.0]), trace=rng.choice([0.95, 1.0, 0.0]),
+                           episode=rng.choice([1000, 30, 5]))
+    classes = rng.choice(TILES) if rng.random() < .4 else _log_int(rng, 1, MOST_CLASSES)
+    few = kind == "loss"                # (a loss reads and writes its rows)
+    rows = _log_int(rng, 1, max(1, min(2097152, MOST_LOGITS // (2 if few else 1) // classes)))
+    more = dict(masked=rng.random() < .5, padded=rng.random() < .25, temperature=rng.choice([1.0, 1.0, 0.7, 1.5]))
+    if few:
+        return _loss(rows, classes, dtype, values=rng.random() < .7, clipped=rng.random() < .8, **more)
+    if rng.random() < .1:
+        more["temperature"] = 0.0       # the best class
+    return _sample(rows, classes, dtype, top_k=rng.choice([0, 0, _log_int(rng, 1, classes)]),
+                   top_p=rng.choice([1.0, 1.0, 0.9, rng.uniform(.1, .99)]), min_p=rng.choice([0.0, 0.0, 0.05, 0.002]), **more)
+
+
+def _logits(case, gen):
+    """Logits of a policy that has learnt something, in rows that may be padded, and the mask of what it may
+    do: a row's allowed classes are the first few (the cells inside a smaller map) without some frozen ones."""
+    n, V, dev = case["rows"], case["classes"], "cuda"
+    wide = V + (PAD if case["padded"] else 0)
+    store = torch.randn((n, wide), generator=gen, device=dev).mul_(1.5).to(DTYPES[case["dtype"]])
+    mask = None
+    if case["masked"]:
+        inside = torch.randint(max(1, V // 4), V + 1, (n, 1), generator=gen, device=dev)
+        mask = (torch.rand((n, V), generator=gen, device=dev) > .02).to(torch.uint8)
+        mask *= torch.arange(V, device=dev)[None] < inside
+        mask *= torch.rand((n, 1), generator=gen, device=dev) > .002      # levels in which nothing may be done
+        mask = mask.contiguous()
+    return store[:, :V], mask
+
+
+def _inputs(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    dev = "cuda"
+    if case["kind"] == "advantages":
+        T, n = case["steps"], case["envs"]
+        reward = torch.randint(-12, 13, (T, n), generator=gen, device=dev).float()
+        reward *= torch.rand((T, n), generator=gen, device=dev) < .5      # edits that changed nothing
+        return dict(reward=reward, done=(torch.rand((T, n), generator=gen, device=dev) < 1 / case["episode"]).to(torch.uint8),
+                    values=torch.randn((T + 1, n), generator=gen, device=dev).mul_(4).add_(10).to(DTYPES[case["dtype"]]))
+    logits, mask = _logits(case, gen)
+    n = case["rows"]
+    s = dict(logits=logits, mask=mask)
+    if case["kind"] == "sample":
+        s["uniform"] = torch.rand((n,), generator=gen, device=dev)
+        return s
+    # the actions of a policy a few updates back, and what it thought of them
+    step = max(1, (64 << 20) // case["classes"])
+    actions, then = [], []
+    for i in range(0, n, step):
+        x = logits[i:i + step].float()
+        x = x + .15 * torch.randn(x.shape, generator=gen, device=dev)
+        if mask is not None:
+            x = x.masked_fill(mask[i:i + step] == 0, -math.inf)
+        p = torch.log_softmax(x / case["temperature"], 1)
+        noise = torch.rand(x.shape, generator=gen, device=dev).clamp_(1e-7).log_().neg_().log_().neg_()
+        best, a = (p + noise).max(1)
+        empty = ~torch.isfinite(x).any(1)
+        actions.append(a.masked_fill(empty, -1).int())
+        then.append(p.gather(1, a[:, None])[:, 0].masked_fill(empty, 0.))
+    s.update(actions=torch.cat(actions), advantages=torch.randn((n,), generator=gen, device=dev), old=None, values=None, returns=None)
+    if case["clipped"]:
+        s["old"] = torch.cat(then)
+    if case["values"]:
+        v = torch.randn((n,), generator=gen, device=dev) * 4
+        s.update(values=v.to(DTYPES[case["dtype"]]), returns=v + torch.randn((n,), generator=gen, device=dev))
+    return s
+
+
+def _scale(case):
+    """One over the rows; a loss that goes on in 16-bit floating point is scaled up as such training does."""
+    return (1024. if case["dtype"] == "float16" else 1.) / case["rows"]
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    s["case"] = case
+    if own:
+        from paper_2408_12525_amd import binding, workloads as wl
+        s["env"] = binding.Pcgrl(wl.make_config(wl.DUNGEON, 64, 32, 15), 0)
+    return s
+
+
+def run(state):
+    case = state["case"]
+    if case["kind"] == "sample":
+        how = dict(temperature=case["temperature"], top_k=case["top_k"], top_p=case["top_p"], min_p=case["min_p"])
+        if own:
+            return state["env"].pcgrl_sample(state["logits"], state["uniform"], mask=state["mask"], **how)
+        return plain_sample(state["logits"], state["uniform"], state["mask"], **how)
+    if case["kind"] == "advantages":
+        args = state["reward"], state["done"], state["values"], case["discount"], case["trace"]
+        return state["env"].pcgrl_advantages(*args) if own else plain_advantages(*args)
+    args = state["logits"], state["actions"], state["advantages"]
+    more = dict(old_log_probs=state["old"], mask=state["mask"], values=state["values"], returns=state["returns"],
+                temperature=case["temperature"], scale=_scale(case), **WEIGHTS)
+    got = state["env"].pcgrl_policy_loss(*args, **more) if own else plain_loss(*args, **more)
+    return {k: v for k, v in got.items() if v is not None}
+
+
+def plain_sample(logits, uniform, mask, temperature, top_k, top_p, min_p):
+    """Actions and log-probabilities.  A class is kept while it is among the top_k largest logits (ties: the
+    lowest index), while the classes before it in that order have less than top_p of the weight that
+    top_k left, and while its weight is at least min_p times the largest.  The action is the first
+    kept class, by index, whose running sum exceeds uniform times the sum (in 64 bits: a uniform
+    number may fall next to a border).  A row in which nothing is allowed has action -1."""
+    n, V = logits.shape
+    x = logits.double()
+    if mask is not None:
+        x = x.masked_fill(mask == 0, -math.inf)
+    most = x.amax(1, keepdim=True)
+    live = torch.isfinite(most)
+    if temperature == 0:
+        at = torch.arange(V, device=x.device)[None]
+        best = torch.where(x == most, at, V).amin(1)
+        return (torch.where(live[:, 0], best, -1).int(), torch.zeros((n,), device=x.device))
+    y = torch.where(live & (x > -math.inf), (x - most) / temperature, -math.inf)
+    w = torch.exp(y)
+    total = w.sum(1)
+    if top_k > 0 or top_p < 1 or min_p > 0:
+        order = torch.sort(x, dim=1, descending=True, stable=True).indices
+        ws = w.gather(1, order)
+        if top_k > 0:
+            ws[:, top_k:] = 0
+        keep = ws >= min_p
+        if top_p < 1:
+            before = ws.cumsum(1)
+            target = top_p * before[:, -1:]
+            keep &= (before - ws) < target
+        kept = torch.zeros_like(w).scatter_(1, order, ws * keep)
+    else:
+        kept = w
+    sums = kept.cumsum(1)
+    action = (sums <= uniform.double()[:, None] * sums[:, -1:]).sum(1)
+    action = torch.where(live[:, 0], action, 0)
+    logp = y.gather(1, action[:, None])[:, 0] - torch.log(total)
+    live = live[:, 0]
+    return torch.where(live, action, -1).int(), torch.where(live, logp, 0.).float()
+
+
+def plain_advantages(reward, done, values, discount, trace):
+    v = values.float()
+    go = 1. - done.float()
+    delta = reward + discount * go * v[1:] - v[:-1]
+    decay = discount * trace * go
+    out = torch.empty_like(delta)
+    a = torch.zeros_like(delta[0])
+    for t in range(len(delta) - 1, -1, -1):
+        a = delta[t] + decay[t] * a
+        out[t] = a
+    return out, out + v[:-1]
+
+
+def plain_loss(logits, actions, advantages, old_log_probs, mask, values, returns, temperature, scale, clip_low, clip_high,
+               entropy_coef, value_coef):
+    """Sums over the rows and gradients of scale * sum(policy loss - entropy_coef * entropy + value_coef *
+    value loss).  Rows whose action is no allowed class count for nothing.  Log-probabilities in 64
+    bits (a ratio may lie next to where it is clipped)."""
+    n, V = logits.shape
+    x = logits.double()
+    if mask is not None:
+        x = x.masked_fill(mask == 0, -math.inf)
+    most = x.amax(1, keepdim=True)
+    some = torch.isfinite(most)
+    y = torch.where(some & (x > -math.inf), (x - most) / temperature, -math.inf)
+    logp = y - torch.log(torch.exp(y).sum(1, keepdim=True))
+    a = actions.long()
+    inside = (a >= 0) & (a < V)
+    a = torch.where(inside, a, 0)
+    own_logp = logp.gather(1, a[:, None])[:, 0]
+    use = inside & some[:, 0] & (own_logp > -math.inf)
+    own_logp = torch.where(use, own_logp, 0.)
+    adv = torch.where(use, advantages, 0.).double()
+    then = own_logp if old_log_probs is None else torch.where(use, old_log_probs, 0.).double()
+    log_ratio = own_logp - then
+    ratio = torch.exp(log_ratio)
+    clipped = ((adv > 0) & (ratio > 1 + clip_high)) | ((adv < 0) & (ratio < 1 - clip_low))
+    if old_log_probs is None:
+        clipped = torch.zeros_like(clipped)
+        policy = -adv * own_logp
+    else:
+        policy = -torch.minimum(ratio * adv, ratio.clamp(1 - clip_low, 1 + clip_high) * adv)
+    p = torch.exp(logp).float()
+    lp = torch.where(p > 0, logp.float(), 0.)
+    entropy = -(p * lp).sum(1)
+    entropy = torch.where(use, entropy, 0.)
+    pull = torch.where(clipped, 0., -adv * ratio).float()
+    g = entropy_coef * p * (lp + entropy[:, None]) - pull[:, None] * p
+    g.scatter_add_(1, a[:, None], pull[:, None])
+    g = torch.where(use[:, None] & (p > 0), g * (scale / temperature), 0.).to(logits.dtype)
+    sums = [use.sum().double(), policy.sum(), entropy.double().sum()]
+    grad_values = None
+    if values is not None:
+        off = torch.where(use, values.double() - returns.double(), 0.)
+        grad_values = (off * (value_coef * scale)).to(values.dtype)
+        sums.append((.5 * off * off).sum())
+    else:
+        sums.append(torch.zeros_like(sums[0]))
+    sums += [torch.where(use, ratio - 1 - log_ratio, 0.).sum(), (clipped & use).sum().double()]
+    loss = scale * (sums[1] - entropy_coef * sums[2] + value_coef * sums[3])
+    return dict(stats=torch.stack([loss] + sums).float(), grad_logits=g, grad_values=grad_values)
+
+
+def work(case):
+    """Bytes and operations that a pass cannot do without."""
+    size = DTYPES[case["dtype"]].itemsize
+    if case["kind"] == "advantages":
+        T, n = case["steps"], case["envs"]
+        return {"bytes": T * n * (4 + 1 + 8) + (T + 1) * n * size, "flops": 8 * T * n}
+    n, V = case["rows"], case["classes"]
+    one = V * size + (V if case["masked"] else 0)
+    if case["kind"] == "sample":
+        return {"bytes": n * (one + 4 + 8), "flops": 6 * n * V}
+    one += V * size + 4 + 4 + (4 if case["clipped"] else 0) + ((2 * size + 4) if case["values"] else 0)
+    return {"bytes": n * one + 28, "flops": 12 * n * V}
+
+
+# ---- the definitions once more, in numpy and 64 bits
+
+def exact(case, seed):
+    s = {k: None if v is None else v.cpu() for k, v in _inputs(case, seed).items()}
+    s = {k: None if v is None else (v.double().numpy() if v.is_floating_point() else v.numpy()) for k, v in s.items()}
+    if case["kind"] == "advantages":
+        return _exact_advantages(case, s)
+    blocks = max(1, -(-case["rows"] * case["classes"] // (8 << 20)))
+    rows = -(-case["rows"] // blocks)
+    cut = lambda k, i: None if s.get(k) is None else s[k][i:i + rows]  # noqa: E731
+    parts = [(_exact_sample if case["kind"] == "sample" else _exact_loss)(case, lambda k, i=i: cut(k, i)) for i in range(0, case["rows"], rows)]
+    if case["kind"] == "sample":
+        return tuple(torch.from_numpy(np.concatenate([p[j] for p in parts])) for j in range(2))
+    sums = sum(p["sums"] for p in parts)
+    loss = _scale(case) * (sums[1] - WEIGHTS["entropy_coef"] * sums[2] + WEIGHTS["value_coef"] * sums[3])
+    out = dict(stats=torch.from_numpy(np.concatenate([[loss], sums])),
+               grad_logits=torch.from_numpy(np.concatenate([p["grad_logits"] for p in parts])))
+    if case["values"]:
+        out["grad_values"] = torch.from_numpy(np.concatenate([p["grad_values"] for p in parts]))
+    return out
+
+
+def _exact_advantages(case, s):
+    T = case["steps"]
+    out, after = np.empty_like(s["reward"]), 0.
+    for t in range(T - 1, -1, -1):
+        goes_on = s["done"][t] == 0
+        error = s["reward"][t] + np.where(goes_on, case["discount"] * s["values"][t + 1], 0.) - s["values"][t]
+        after = error + np.where(goes_on, case["discount"] * case["trace"] * after, 0.)
+        out[t] = after
+    return torch.from_numpy(out), torch.from_numpy(out + s["values"][:T])
+
+
+def _shares(case, of):
+    """exp of (logit - largest) / temperature, 0 where not allowed, and whether a row allows anything."""
+    x = of("logits")
+    allowed = np.isfinite(x) if of("mask") is None else np.isfinite(x) & (of("mask") != 0)
+    x = np.where(allowed, x, -np.inf)
+    live = allowed.any(1)
+    top = np.where(live, x.max(1), 0.)
+    return x, live, top, np.exp((x - top[:, None]) / (case["temperature"] or 1.))
+
+
+def _exact_sample(case, of):
+    x, live, top, w = _shares(case, of)
+    n, V = x.shape
+    if case["temperature"] == 0:
+        return np.where(live, x.argmax(1), -1).astype(np.int32), np.zeros(n)
+    kept = w
+    if case["top_k"] or case["top_p"] < 1 or case["min_p"] > 0:
+        order = np.argsort(-x, axis=1, kind="stable")
+        falling = np.take_along_axis(w, order, 1)
+        running = np.cumsum(falling, 1)
+        count = np.full(n, min(case["top_k"] or V, V))
+        if case["top_p"] < 1:               # as many as it takes for the sum to reach the share
+            whole = running[np.arange(n), count - 1]
+            count = np.minimum(count, 1 + (running < (case["top_p"] * whole)[:, None]).sum(1))
+        count = np.minimum(count, (falling >= case["min_p"]).sum(1))
+        rank = np.empty_like(order)
+        np.put_along_axis(rank, order, np.broadcast_to(np.arange(V), (n, V)), 1)
+        kept = np.where(rank < count[:, None], w, 0.)
+    running = np.cumsum(kept, 1)
+    action = (running > (of("uniform") * running[:, -1])[:, None]).argmax(1)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        logp = (x[np.arange(n), action] - top) / case["temperature"] - np.log(w.sum(1))
+    return np.where(live, action, -1).astype(np.int32), np.where(live, logp, 0.)
+
+
+def _exact_loss(case, of):
+    x, live, top, w = _shares(case, of)
+    n, V = x.shape
+    T, c, rows = case["temperature"], WEIGHTS, np.arange(n)
+    a = of("actions")
+    use = live & (a >= 0) & (a < V)
+    a = np.where(use, a, 0)
+    use &= w[rows, a] > 0
+    whole = np.where(live, w.sum(1), 1.)
+    p = w / whole[:, None]
+    now = np.where(use, (np.where(use, x[rows, a], 0.) - top) / T - np.log(whole), 0.)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        logs = np.where(p > 0, (x - top[:, None]) / T - np.log(whole)[:, None], 0.)
+    entropy = np.where(use, -(p * logs).sum(1), 0.)
+    adv = np.where(use, of("advantages"), 0.)
+    change = now - np.where(use, of("old"), 0.) if case["clipped"] else np.zeros(n)
+    ratio = np.exp(change)
+    if case["clipped"]:
+        held = np.where(adv > 0, ratio > 1 + c["clip_high"], ratio < 1 - c["clip_low"]) & (adv != 0)
+        policy = -adv * np.where(held, np.where(adv > 0, 1 + c["clip_high"], 1 - c["clip_low"]), ratio)
+    else:
+        held, policy = np.zeros(n, bool), -adv * now
+    chosen = np.zeros_like(p)
+    chosen[rows, a] = 1.
+    g = np.where(held, 0., -adv * ratio)[:, None] * (chosen - p) + c["entropy_coef"] * p * (logs + entropy[:, None])
+    out = dict(grad_logits=g * (use * _scale(case) / T)[:, None])
+    sums = [use.sum(), policy.sum(), entropy.sum(), 0., np.where(use, ratio - 1 - change, 0.).sum(), (held & use).sum()]
+    if case["values"]:
+        off = np.where(use, of("values") - of("returns"), 0.)
+        out["grad_values"] = off * c["value_coef"] * _scale(case)
+        sums[3] = (off * off).sum() / 2
+    out["sums"] = np.array(sums, float)
+    return out
