@@ -194,17 +194,19 @@ def plain_sample(logits, uniform, mask, temperature, top_k, top_p, min_p):
     lowest index), while the classes before it in that order have less than top_p of the weight that
     top_k left, and while its weight is at least min_p times the largest.  The action is the first
     kept class, by index, whose running sum exceeds uniform times the sum (in 64 bits: a uniform
-    number may fall next to a border).  A row in which nothing is allowed has action -1."""
+    number may fall next to a border).  A row in which nothing is allowed has action -1 and
+    log-probability 0, one with a NaN or +infinity among what is allowed action -1 and NaN."""
     n, V = logits.shape
     x = logits.double()
     if mask is not None:
         x = x.masked_fill(mask == 0, -math.inf)
     most = x.amax(1, keepdim=True)
     live = torch.isfinite(most)
+    dead = torch.where(most[:, 0] == -math.inf, 0., math.nan)
     if temperature == 0:
         at = torch.arange(V, device=x.device)[None]
         best = torch.where(x == most, at, V).amin(1)
-        return (torch.where(live[:, 0], best, -1).int(), torch.zeros((n,), device=x.device))
+        return torch.where(live[:, 0], best, -1).int(), torch.where(live[:, 0], 0., dead).float()
     y = torch.where(live & (x > -math.inf), (x - most) / temperature, -math.inf)
     w = torch.exp(y)
     total = w.sum(1)
@@ -226,7 +228,7 @@ def plain_sample(logits, uniform, mask, temperature, top_k, top_p, min_p):
     action = torch.where(live[:, 0], action, 0)
     logp = y.gather(1, action[:, None])[:, 0] - torch.log(total)
     live = live[:, 0]
-    return torch.where(live, action, -1).int(), torch.where(live, logp, 0.).float()
+    return torch.where(live, action, -1).int(), torch.where(live, logp, dead).float()
 
 
 def plain_advantages(reward, done, values, discount, trace):
@@ -245,21 +247,22 @@ def plain_advantages(reward, done, values, discount, trace):
 def plain_loss(logits, actions, advantages, old_log_probs, mask, values, returns, temperature, scale, clip_low, clip_high,
                entropy_coef, value_coef):
     """Sums over the rows and gradients of scale * sum(policy loss - entropy_coef * entropy + value_coef *
-    value loss).  Rows whose action is no allowed class count for nothing.  Log-probabilities in 64
-    bits (a ratio may lie next to where it is clipped)."""
+    value loss).  Rows whose action is no allowed class count for nothing, NaN and +infinity among
+    what is allowed make theirs NaN.  Log-probabilities in 64 bits (a ratio may lie next to where it
+    is clipped)."""
     n, V = logits.shape
     x = logits.double()
     if mask is not None:
         x = x.masked_fill(mask == 0, -math.inf)
     most = x.amax(1, keepdim=True)
-    some = torch.isfinite(most)
-    y = torch.where(some & (x > -math.inf), (x - most) / temperature, -math.inf)
+    some = most != -math.inf
+    y = torch.where(some & (x != -math.inf), (x - most) / temperature, -math.inf)
     logp = y - torch.log(torch.exp(y).sum(1, keepdim=True))
     a = actions.long()
     inside = (a >= 0) & (a < V)
     a = torch.where(inside, a, 0)
     own_logp = logp.gather(1, a[:, None])[:, 0]
-    use = inside & some[:, 0] & (own_logp > -math.inf)
+    use = inside & some[:, 0] & (own_logp != -math.inf)
     own_logp = torch.where(use, own_logp, 0.)
     adv = torch.where(use, advantages, 0.).double()
     then = own_logp if old_log_probs is None else torch.where(use, old_log_probs, 0.).double()
@@ -272,13 +275,13 @@ def plain_loss(logits, actions, advantages, old_log_probs, mask, values, returns
     else:
         policy = -torch.minimum(ratio * adv, ratio.clamp(1 - clip_low, 1 + clip_high) * adv)
     p = torch.exp(logp).float()
-    lp = torch.where(p > 0, logp.float(), 0.)
+    lp = torch.where(p != 0, logp.float(), 0.)
     entropy = -(p * lp).sum(1)
     entropy = torch.where(use, entropy, 0.)
     pull = torch.where(clipped, 0., -adv * ratio).float()
     g = entropy_coef * p * (lp + entropy[:, None]) - pull[:, None] * p
     g.scatter_add_(1, a[:, None], pull[:, None])
-    g = torch.where(use[:, None] & (p > 0), g * (scale / temperature), 0.).to(logits.dtype)
+    g = torch.where(use[:, None] & (p != 0), g * (scale / temperature), 0.).to(logits.dtype)
     sums = [use.sum().double(), policy.sum(), entropy.double().sum()]
     grad_values = None
     if values is not None:
