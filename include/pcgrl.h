@@ -310,6 +310,123 @@ int pcgrl_bad_action_count(pcgrl_ctx* ctx, uint64_t* out, void* stream);
 #define PCGRL_UNPACK_F32 3
 int pcgrl_unpack_obs(const pcgrl_ctx* ctx, const uint8_t* packed, void* out, int32_t out_type, void* stream);
 
+/* ---- The policy's side: what a training loop computes between an environment's steps.
+ *
+ * The calls below take a context only for its device; they neither read nor change its environments
+ * (pcgrl_step_logits excepted), keep nothing from one call to the next, allocate nothing and may be captured
+ * into a HIP graph.  Different calls may run at the same time on different streams.  Element types:
+ * PCGRL_UNPACK_F16 / _BF16 / _F32.  Every array is aligned to its element size.
+ *
+ * Logits have one row for each decision and one class for each choice: a tile type for the agent's cell
+ * (as pcgrl_step takes it), or a cell and a tile type for a policy that chooses both.  A class may
+ * be chosen if its mask byte is not 0 (mask NULL: all) and its logit is not -infinity.  Logits, values
+ * and other numbers that masked classes hold are not looked at. */
+#define PCGRL_MAX_CLASSES 32768
+
+typedef struct {
+  int32_t type;          /* of the logits */
+  int32_t n_classes;     /* 1..PCGRL_MAX_CLASSES */
+  int64_t logits_stride; /* elements from one row of logits to the next, >= n_classes (any for one row) */
+  int64_t mask_stride;   /* bytes from one row of the mask to the next, >= n_classes; 0 = one row for all */
+  double temperature;    /* 0 = the largest logit; or 1e-30 .. 3e38 */
+  double top_p;          /* > 0; 1 or more = off */
+  double min_p;          /* 0..1; 0 = off */
+  int32_t top_k;         /* >= 0; 0 = off */
+} pcgrl_sampling;
+
+/* Draws one class for each row (Methods / Training: the agent acts by its policy) from given
+ * uniform numbers.  With w = exp((logit - largest logit) / temperature), and the classes ordered by falling
+ * logit, equal ones by index, a class is kept while it is among the first top_k, while the sum of the
+ * weights before it is below top_p times the sum of what top_k left, and while w >= min_p.  The
+ * action is the first kept class, by index, at which the running sum of the kept weights exceeds
+ * uniform times their sum; weights are rounded to 2^-39 of the largest or finer, and summed exactly.
+ *   logits   : device, [n_rows][logits_stride] elements
+ *   mask     : device, uint8 [n_rows][mask_stride], or NULL
+ *   uniform  : device, float32 [n_rows] in [0, 1) (what is outside or NaN counts as the nearest such number,
+ *              NaN as 0); may be NULL if temperature is 0
+ *   actions  : device, int32 [n_rows]; -1 for a row in which nothing may be chosen, or in which a
+ *              class that may be chosen has the logit NaN or +infinity (pcgrl_step counts -1 as a bad action)
+ *   log_probs: device, float32 [n_rows], or NULL: log-probability of the action under the policy, that is
+ *              with mask and temperature, without top_k, top_p and min_p (the policy that
+ *              pcgrl_policy_loss differentiates); 0 at temperature 0 and where nothing may be chosen, NaN
+ *              where a logit is NaN or +infinity
+ * Errors: E_NULL; E_CONFIG if a field of *how or n_rows is out of range or a pointer is misaligned. */
+int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask,
+                 const float* uniform, int64_t n_rows, int32_t* actions, float* log_probs, void* stream);
+
+/* pcgrl_sample for every environment, and pcgrl_step with the actions drawn: a step of a policy in the
+ * loop as one call (Methods / Training).  n_classes must be the number of tile types, n_rows is the
+ * batch; actions is required (and written), log_probs, obs, reward and done may be NULL.
+ * Errors: those of both. */
+int pcgrl_step_logits(pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask,
+                      const float* uniform, int32_t* actions, float* log_probs, uint8_t* obs, float* reward,
+                      uint8_t* done, void* stream);
+
+/* Generalised advantages of a rollout and the returns that go with them (Methods / Training: the
+ * training algorithm), backwards over the steps of each environment, from what pcgrl_rollout or
+ * n_steps calls of pcgrl_step wrote and the values of a critic:
+ *   error(t)     = reward(t) + discount * value(t + 1) - value(t)
+ *   advantage(t) = error(t) + discount * trace * advantage(t + 1),   return(t) = advantage(t) + value(t)
+ * where done(t) is not 0, value(t + 1) and advantage(t + 1) count as 0, whatever they hold; beyond the last
+ * step the advantage is 0.  Summed in 64 bits.
+ *   reward: device, float32 [n_steps][n_envs]; done: device, uint8 [n_steps][n_envs]
+ *   values: device, [n_steps + 1][n_envs] elements of values_type, the last row for the observations
+ *           after the last step
+ *   advantages: device, float32 [n_steps][n_envs]; returns: the same, or NULL.  Neither may overlap an input.
+ * n_steps is 0..2^20, n_envs 0..2^24, discount and trace 0..1.
+ * Errors: E_NULL; E_CONFIG if a number is out of range or a pointer is misaligned. */
+int pcgrl_advantages(const pcgrl_ctx* ctx, const float* reward, const uint8_t* done, const void* values,
+                     int32_t values_type, int32_t n_steps, int32_t n_envs, double discount, double trace,
+                     float* advantages, float* returns, void* stream);
+
+typedef struct {
+  int32_t type;                /* of logits, values, grad_logits and grad_values */
+  int32_t n_classes;           /* 1..PCGRL_MAX_CLASSES */
+  int64_t n_rows;              /* >= 0 */
+  const void* logits;          /* [n_rows][logits_stride] */
+  int64_t logits_stride;       /* elements, >= n_classes (any for one row) */
+  const uint8_t* mask;         /* [n_rows][mask_stride], or NULL */
+  int64_t mask_stride;         /* bytes, >= n_classes; 0 = one row for all */
+  const int32_t* actions;      /* [n_rows]; a row whose action is no class that may be chosen is not counted */
+  const float* advantages;     /* [n_rows] */
+  const float* old_log_probs;  /* [n_rows] of the policy that acted, or NULL: no ratio, nothing is clipped */
+  const void* values;          /* [n_rows], or NULL: no value loss */
+  const float* returns;        /* [n_rows], required with values */
+  double temperature;          /* 1e-30 .. 3e38 */
+  double clip_low, clip_high;  /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; 0..1 and >= 0 */
+  double entropy_coef, value_coef;
+  double scale;                /* of the loss and its gradients, e.g. 1 / rows (more for float16) */
+  void* grad_logits;           /* [n_rows][grad_stride], or NULL; may be `logits` itself, with its stride */
+  int64_t grad_stride;         /* elements, >= n_classes (any for one row) */
+  void* grad_values;           /* [n_rows], or NULL; may be `values` itself */
+  float* log_probs;            /* [n_rows], or NULL: log-probabilities of the actions (0 if not counted) */
+  float* entropies;            /* [n_rows], or NULL: entropies of the rows (0 if not counted) */
+  float* stats;                /* [PCGRL_LOSS_STATS], or NULL */
+  void* workspace;             /* pcgrl_policy_loss_workspace() bytes, 8-byte aligned, required with stats; used
+                                  by one call at a time, and free for other uses when its kernels have run */
+} pcgrl_loss;
+
+/* stats: the loss, then sums over the rows counted (neither scaled nor weighted): their number, policy loss,
+ * entropy, value loss, ratio - 1 - log ratio (an estimate of the divergence from the old policy), clipped rows */
+#define PCGRL_LOSS_STATS 7
+
+/* The clipped policy loss with an entropy bonus and a value loss, and its gradients (Methods /
+ * Training: the training algorithm).  All pointers in *loss are device pointers.  With p the softmax of
+ * logits / temperature over the classes that may be chosen, r = p(action) / exp(old_log_prob), A the
+ * advantage and H the entropy of p:
+ *   loss = scale * sum over rows of ( -min(r A, clip(r) A) - entropy_coef H + value_coef (value - return)^2 / 2 )
+ * and with old_log_probs NULL -A log p(action) in place of the minimum (with A = 1 the cross entropy).
+ *   d loss / d logit(j)  = scale / temperature * ( u (1[j = action] - p(j)) + entropy_coef p(j) (log p(j) + H) ),
+ *                          u = -A r (r = 1 with old_log_probs NULL), 0 where the clipped branch is the smaller
+ *   d loss / d value     = scale * value_coef * (value - return)
+ * Gradients are written, not added: 0 where a class may not be chosen and in rows that are not counted
+ * (their advantages, old_log_probs, values and returns are not looked at).  A row counted with a NaN or +infinity
+ * among the logits that may be chosen has NaN for gradients.  Elements behind a row's classes are left alone.
+ * Probabilities are summed, and ratios compared, in 64 bits; stats are the same from call to call.
+ * Errors: E_NULL; E_CONFIG if a field is out of range or a pointer is misaligned. */
+int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* loss, void* stream);
+int64_t pcgrl_policy_loss_workspace(void); /* bytes; host side, no GPU work */
+
 /* Measurement aid (no passage of the paper: it is the yardstick its store-bound steps are held
  * against).  One launch that does nothing but write n_regions * region_bytes bytes to dst with
  * aligned 16-byte stores of the kind `store_mode` names (PCGRL_OBS_STORE_CACHED / _STREAM /

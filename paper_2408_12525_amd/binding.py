@@ -47,12 +47,35 @@ class PcgrlConfig(C.Structure):
     ]
 
 
+class PcgrlSampling(C.Structure):
+    _fields_ = [
+        ("type", C.c_int32), ("n_classes", C.c_int32), ("logits_stride", C.c_int64), ("mask_stride", C.c_int64),
+        ("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
+    ]
+
+
+class PcgrlLoss(C.Structure):
+    _fields_ = [
+        ("type", C.c_int32), ("n_classes", C.c_int32), ("n_rows", C.c_int64),
+        ("logits", C.c_void_p), ("logits_stride", C.c_int64), ("mask", C.c_void_p), ("mask_stride", C.c_int64),
+        ("actions", C.c_void_p), ("advantages", C.c_void_p), ("old_log_probs", C.c_void_p),
+        ("values", C.c_void_p), ("returns", C.c_void_p),
+        ("temperature", C.c_double), ("clip_low", C.c_double), ("clip_high", C.c_double),
+        ("entropy_coef", C.c_double), ("value_coef", C.c_double), ("scale", C.c_double),
+        ("grad_logits", C.c_void_p), ("grad_stride", C.c_int64), ("grad_values", C.c_void_p),
+        ("log_probs", C.c_void_p), ("entropies", C.c_void_p), ("stats", C.c_void_p), ("workspace", C.c_void_p),
+    ]
+
+
+LOSS_STATS = 7  # the loss, rows counted, then sums over them: policy loss, entropy, value loss, divergence, clipped rows
+
 EXPORTS = [
     "pcgrl_config_default", "pcgrl_create", "pcgrl_destroy", "pcgrl_reset", "pcgrl_step", "pcgrl_rollout",
     "pcgrl_metrics", "pcgrl_exact_diameter", "pcgrl_exact_diameter_static", "pcgrl_observe", "pcgrl_get_state", "pcgrl_set_state", "pcgrl_set_targets",
     "pcgrl_get_targets",
     "pcgrl_obs_shape", "pcgrl_obs_bytes", "pcgrl_obs_stride", "pcgrl_num_metrics", "pcgrl_num_tiles", "pcgrl_bad_action_count",
     "pcgrl_selftest", "pcgrl_store_rate", "pcgrl_unpack_obs", "pcgrl_strerror",
+    "pcgrl_sample", "pcgrl_step_logits", "pcgrl_advantages", "pcgrl_policy_loss", "pcgrl_policy_loss_workspace",
 ]
 
 _lib = None
@@ -108,6 +131,13 @@ def load():
     L.pcgrl_selftest.argtypes = [C.c_int, C.POINTER(i32)]
     L.pcgrl_store_rate.argtypes = [p, C.c_int64, i32, i32, i32, p]
     L.pcgrl_unpack_obs.argtypes = [p, p, p, i32, p]
+    i64, f64 = C.c_int64, C.c_double
+    L.pcgrl_sample.argtypes = [p, C.POINTER(PcgrlSampling), p, p, p, i64, p, p, p]
+    L.pcgrl_step_logits.argtypes = [p, C.POINTER(PcgrlSampling), p, p, p, p, p, p, p, p, p]
+    L.pcgrl_advantages.argtypes = [p, p, p, p, i32, i32, i32, f64, f64, p, p, p]
+    L.pcgrl_policy_loss.argtypes = [p, C.POINTER(PcgrlLoss), p]
+    L.pcgrl_policy_loss_workspace.argtypes = []
+    L.pcgrl_policy_loss_workspace.restype = i64
     L.pcgrl_strerror.argtypes = [C.c_int]
     L.pcgrl_strerror.restype = C.c_char_p
     _lib = L
@@ -375,6 +405,130 @@ class Pcgrl:
         o = self._dev(out, torch.int32, (self.B, self.M, 2), "out")
         _check(self.L.pcgrl_get_targets(self.h, o, self._st()), "pcgrl_get_targets")
         return out
+
+    # -- the policy's side (any number of rows; the context says which GPU)
+    LOGIT_TYPES = {torch.float16: 1, torch.bfloat16: 2, torch.float32: 3}
+
+    def _type(self, t, name):
+        if not isinstance(t, torch.Tensor) or t.dtype not in self.LOGIT_TYPES:
+            raise PcgrlError(f"{name} must be a float16, bfloat16 or float32 tensor")
+        return self.LOGIT_TYPES[t.dtype]
+
+    def _rows(self, t, dtypes, shape, name, one_for_all=False):
+        """Pointer and row stride of a matrix whose rows are contiguous and may lie apart."""
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == self.device):
+            raise PcgrlError(f"{name} must be a tensor on {self.device}")
+        if one_for_all and t.dim() == 1:
+            t = t[None].expand(shape)
+        if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)) or t.dtype not in dtypes:
+            raise PcgrlError(f"{name} must be {' or '.join(map(str, dtypes))} of shape "
+                             f"{tuple(shape) if shape is not None else '[rows, classes]'}, got {t.dtype} {tuple(t.shape)}")
+        n, V = t.shape
+        if (V > 1 and t.stride(1) != 1) or (n > 1 and t.stride(0) < V and not (one_for_all and t.stride(0) == 0)):
+            raise PcgrlError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
+        return C.c_void_p(t.data_ptr()), (t.stride(0) if n > 1 else V)
+
+    def _sampling(self, logits, uniform, mask, n_rows, temperature, top_k, top_p, min_p):
+        how = PcgrlSampling(type=self._type(logits, "logits"), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+        x, how.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
+        n, how.n_classes = logits.shape
+        if n_rows is not None and n != n_rows:
+            raise PcgrlError(f"logits must have a row for each of the {n_rows} environments, got {n}")
+        m = None
+        if mask is not None:
+            m, how.mask_stride = self._rows(mask, (torch.uint8, torch.bool), logits.shape, "mask", one_for_all=True)
+        u = self._dev(uniform, torch.float32, (n,), "uniform", optional=temperature == 0)
+        return how, x, m, u, n
+
+    def pcgrl_sample(self, logits, uniform, mask=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, actions=None, log_probs=None):
+        """Actions [n] int32 drawn from logits [n, classes] with the uniform numbers [n] float32, and their
+        log-probabilities [n] float32 under the policy (mask and temperature, without the truncations).
+        Rows of logits may lie apart; mask [n, classes] or [classes] uint8 or bool."""
+        how, x, m, u, n = self._sampling(logits, uniform, mask, None, temperature, top_k, top_p, min_p)
+        if actions is None:
+            actions = torch.empty((n,), dtype=torch.int32, device=self.device)
+        if log_probs is None:
+            log_probs = torch.empty((n,), dtype=torch.float32, device=self.device)
+        a = self._dev(actions, torch.int32, (n,), "actions")
+        lp = self._dev(log_probs, torch.float32, (n,), "log_probs")
+        _check(self.L.pcgrl_sample(self.h, C.byref(how), x, m, u, n, a, lp, self._st()), "pcgrl_sample")
+        return actions, log_probs
+
+    def pcgrl_step_logits(self, logits, uniform, obs=None, reward=None, done=None, mask=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                          actions=None, log_probs=None):
+        """pcgrl_sample for every environment and pcgrl_step with the actions drawn; returns what
+        pcgrl_sample does."""
+        how, x, m, u, n = self._sampling(logits, uniform, mask, self.B, temperature, top_k, top_p, min_p)
+        if actions is None:
+            actions = torch.empty((n,), dtype=torch.int32, device=self.device)
+        if log_probs is None:
+            log_probs = torch.empty((n,), dtype=torch.float32, device=self.device)
+        a = self._dev(actions, torch.int32, (n,), "actions")
+        lp = self._dev(log_probs, torch.float32, (n,), "log_probs")
+        o = self._dev(obs, torch.uint8, self.obs_shape, "obs", optional=True)
+        r = self._dev(reward, torch.float32, (n,), "reward", optional=True)
+        d = self._dev(done, torch.uint8, (n,), "done", optional=True)
+        _check(self.L.pcgrl_step_logits(self.h, C.byref(how), x, m, u, a, lp, o, r, d, self._st()), "pcgrl_step_logits")
+        return actions, log_probs
+
+    def pcgrl_advantages(self, reward, done, values, discount, trace, advantages=None, returns=None):
+        """Generalised advantages and returns [T, n] float32 of a rollout: reward [T, n] float32, done [T, n]
+        uint8 or bool, values [T + 1, n] float16, bfloat16 or float32."""
+        code = self._type(values, "values")
+        if not isinstance(reward, torch.Tensor) or reward.dim() != 2:
+            raise PcgrlError("reward must be a [steps, environments] tensor")
+        T, n = shape = tuple(reward.shape)
+        r = self._dev(reward, torch.float32, shape, "reward")
+        d = self._dev(done, torch.bool if getattr(done, "dtype", None) == torch.bool else torch.uint8, shape, "done")
+        v = self._dev(values, values.dtype, (T + 1, n), "values")
+        if advantages is None:
+            advantages = torch.empty(shape, dtype=torch.float32, device=self.device)
+        if returns is None:
+            returns = torch.empty(shape, dtype=torch.float32, device=self.device)
+        a = self._dev(advantages, torch.float32, shape, "advantages")
+        q = self._dev(returns, torch.float32, shape, "returns")
+        _check(self.L.pcgrl_advantages(self.h, r, d, v, code, T, n, discount, trace, a, q, self._st()), "pcgrl_advantages")
+        return advantages, returns
+
+    def pcgrl_policy_loss(self, logits, actions, advantages, old_log_probs=None, mask=None, values=None, returns=None, temperature=1.0,
+                          clip_low=0.2, clip_high=0.2, entropy_coef=0.01, value_coef=0.5, scale=None, grad_logits=None,
+                          grad_values=None, log_probs=None, entropies=None, stats=None, workspace=None):
+        """The clipped policy loss of logits [n, classes] and its gradients, as a dict: `stats` (LOSS_STATS
+        float32), `grad_logits` and, with values, `grad_values`, made here where no tensor is given.  The
+        gradients are for logits.backward(grad_logits) or torch.autograd.backward; grad_logits may be
+        the logits.  log_probs and entropies [n] float32 are written if given.  scale: default 1 / n."""
+        l = PcgrlLoss(type=self._type(logits, "logits"), temperature=temperature, clip_low=clip_low, clip_high=clip_high,
+                      entropy_coef=entropy_coef, value_coef=value_coef)
+        l.logits, l.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
+        n, V = logits.shape
+        l.n_rows, l.n_classes, l.scale = n, V, 1 / max(n, 1) if scale is None else scale
+        if mask is not None:
+            l.mask, l.mask_stride = self._rows(mask, (torch.uint8, torch.bool), (n, V), "mask", one_for_all=True)
+        f32 = torch.float32
+        l.actions = self._dev(actions, torch.int32, (n,), "actions")
+        l.advantages = self._dev(advantages, f32, (n,), "advantages")
+        l.old_log_probs = self._dev(old_log_probs, f32, (n,), "old_log_probs", optional=True)
+        l.values = self._dev(values, logits.dtype, (n,), "values", optional=True)
+        l.returns = self._dev(returns, f32, (n,), "returns", optional=values is None)
+        if grad_logits is None:
+            grad_logits = torch.empty((n, V), dtype=logits.dtype, device=self.device)
+        l.grad_logits, l.grad_stride = self._rows(grad_logits, (logits.dtype,), (n, V), "grad_logits")
+        if values is not None and grad_values is None:
+            grad_values = torch.empty((n,), dtype=logits.dtype, device=self.device)
+        l.grad_values = self._dev(grad_values, logits.dtype, (n,), "grad_values", optional=True)
+        l.log_probs = self._dev(log_probs, f32, (n,), "log_probs", optional=True)
+        l.entropies = self._dev(entropies, f32, (n,), "entropies", optional=True)
+        if stats is None:
+            stats = torch.empty((LOSS_STATS,), dtype=f32, device=self.device)
+        l.stats = self._dev(stats, f32, (LOSS_STATS,), "stats")
+        size = self.L.pcgrl_policy_loss_workspace()
+        if workspace is None:
+            workspace = torch.empty((size,), dtype=torch.uint8, device=self.device)
+        elif not isinstance(workspace, torch.Tensor) or workspace.numel() < size:
+            raise PcgrlError(f"workspace must hold {size} bytes")
+        l.workspace = self._dev(workspace, torch.uint8, tuple(workspace.shape), "workspace")
+        _check(self.L.pcgrl_policy_loss(self.h, C.byref(l), self._st()), "pcgrl_policy_loss")
+        return dict(stats=stats, grad_logits=grad_logits, grad_values=grad_values)
 
     def pcgrl_bad_action_count(self) -> int:
         n = C.c_uint64(0)

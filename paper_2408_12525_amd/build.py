@@ -12,7 +12,8 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "pcgrl_api.hip")
-DEPS = [SRC, os.path.join(HERE, "csrc", "pcgrl_kernels.hip.h"), os.path.join(HERE, "csrc", "pcgrl_index.h"),
+POLICY_SRC = os.path.join(HERE, "csrc", "pcgrl_policy.hip")
+DEPS = [SRC, POLICY_SRC, os.path.join(HERE, "csrc", "pcgrl_policy.hip.h"), os.path.join(HERE, "csrc", "pcgrl_host.h"), os.path.join(HERE, "csrc", "pcgrl_kernels.hip.h"), os.path.join(HERE, "csrc", "pcgrl_index.h"),
         os.path.join(HERE, "csrc", "pcgrl_relay.h"), os.path.join(HERE, "csrc", "pcgrl_spans.h"),
         os.path.join(HERE, "csrc", "pcgrl_split.h"),
         os.path.join(os.path.dirname(HERE), "include", "pcgrl.h")]
@@ -21,7 +22,7 @@ LIB = os.path.join(LIB_DIR, "libpcgrl.so")
 PY_SRC = os.path.join(HERE, "csrc", "pcgrl_py.cpp")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # keep hipcc from forming packed fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # the reward is a sum of float32 products in a fixed order: no fused multiply-adds
@@ -118,17 +119,30 @@ def build(force: bool = True, verbose: bool = False) -> str:
         tmp = tempfile.mkdtemp(prefix="pcgrl_build_")
         try:
             out = os.path.join(tmp, "libpcgrl.so")
-            cmd = [hipcc] + HIPCC_FLAGS + ["-save-temps", "-o", out, SRC]
-            if verbose:
-                print(" ".join(cmd), flush=True)
+            parts = []                                  # the translation units, compiled side by side
+            for src in (SRC, POLICY_SRC):
+                name = os.path.splitext(os.path.basename(src))[0]
+                cmd = [hipcc] + HIPCC_FLAGS + ["-save-temps", "-c", "-o", os.path.join(tmp, name + ".o"), src]
+                if verbose:
+                    print(" ".join(cmd), flush=True)
+                log = open(os.path.join(tmp, name + ".log"), "w+")
+                parts.append((name, log, subprocess.Popen(cmd, cwd=tmp, stdout=log, stderr=subprocess.STDOUT)))
+            failed = [name for name, _, p in parts if p.wait() != 0]
+            text = ""
+            for name, log, _ in parts:
+                log.seek(0)
+                if name in failed:
+                    raise RuntimeError("hipcc failed:\n" + log.read())
+                log.close()
+                asm = [f for f in os.listdir(tmp) if f.startswith(name + "-hip") and f.endswith("gfx950.s")]
+                if len(asm) != 1:
+                    raise RuntimeError("device assembly not found among the compiler's temporaries: %s" % os.listdir(tmp))
+                with open(os.path.join(tmp, asm[0])) as f:
+                    text += f.read()
+            cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-o", out] + [os.path.join(tmp, name + ".o") for name, _, _ in parts]
             res = subprocess.run(cmd, cwd=tmp, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
             if res.returncode != 0:
-                raise RuntimeError("hipcc failed:\n" + res.stdout)
-            asm = [f for f in os.listdir(tmp) if f.endswith("gfx950.s")]
-            if len(asm) != 1:
-                raise RuntimeError("device assembly not found among the compiler's temporaries: %s" % os.listdir(tmp))
-            with open(os.path.join(tmp, asm[0])) as f:
-                text = f.read()
+                raise RuntimeError("hipcc failed to link:\n" + res.stdout)
             n_kernels, found = scan_shift_amounts(text)
             with open(SCAN_REPORT, "w") as f:
                 json.dump({"kernels": n_kernels, "findings": found, "resources": kernel_resources(text)}, f)

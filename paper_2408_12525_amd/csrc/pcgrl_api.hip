@@ -7,6 +7,7 @@
 #include <cstring>
 #include <new>
 
+#include "pcgrl_host.h"
 #include "pcgrl_kernels.hip.h"
 #include "pcgrl_spans.h"
 
@@ -48,18 +49,6 @@ struct pcgrl_ctx {
 };
 
 namespace {
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    ok = hipSetDevice(dev) == hipSuccess;
-  }
-  ~DeviceGuard() {
-    if (prev >= 0) (void)hipSetDevice(prev);
-  }
-};
 
 int tiles_of(int problem) { return problem == PCGRL_BINARY ? 2 : problem == PCGRL_MAZE ? 4 : problem == PCGRL_DUNGEON ? 7 : 0; }
 int planes_of(int problem) { return problem == PCGRL_BINARY ? 1 : problem == PCGRL_MAZE ? 2 : 3; }
@@ -321,6 +310,10 @@ int step_store_kind(pcgrl_ctx* ctx, const uint8_t* obs) {
 }
 
 }  // namespace
+
+int pcgrl::device_of(const pcgrl_ctx* ctx) { return ctx->device; }
+int pcgrl::tiles_in(const pcgrl_ctx* ctx) { return ctx->K; }
+int pcgrl::levels_of(const pcgrl_ctx* ctx) { return ctx->cfg.batch; }
 
 extern "C" {
 

@@ -1,0 +1,206 @@
+// Host side of the policy's entry points in include/pcgrl.h: argument checks and launches.
+#include "../../include/pcgrl.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "pcgrl_host.h"
+#include "pcgrl_policy.hip.h"
+
+using namespace pcgrl;
+
+namespace {
+
+int size_of(int type) { return type == PCGRL_UNPACK_F32 ? 4 : type == PCGRL_UNPACK_F16 || type == PCGRL_UNPACK_BF16 ? 2 : 0; }
+bool misaligned(const void* p, int size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) != 0; }
+// Rows of n elements, `stride` apart.
+bool bad_rows(int64_t rows, int64_t stride, int n) { return rows > 1 && (stride < n || stride > ((int64_t)1 << 40)); }
+
+// Bytes of `rows` rows, and whether two stretches of memory share any.
+size_t span(int64_t rows, int64_t stride, int64_t n, int size) { return rows < 1 ? 0 : (size_t)((rows - 1) * stride + n) * size; }
+bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return p && q && a < b + nq && b < a + np;
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? PCGRL_OK : PCGRL_E_HIP; }
+
+// Calls f with the type and with the team and the classes a thread of the smallest team that holds a row.
+template <int TEAM, int PER> struct Shape {
+  static constexpr int kTeam = TEAM, kPer = PER;
+};
+template <typename F> int by_type(int type, F&& f) {
+  if (type == PCGRL_UNPACK_F32) return f(F32{});
+  if (type == PCGRL_UNPACK_F16) return f(F16{});
+  return f(BF16{});
+}
+template <typename F> int by_classes(int n, F&& f) {
+  if (n <= 8) return f(Shape<1, 8>{});
+  if (n <= 64) return f(Shape<8, 8>{});
+  if (n <= 512) return f(Shape<64, 8>{});
+  if (n <= 2048) return f(Shape<256, 8>{});
+  if (n <= 8192) return f(Shape<256, 32>{});
+  if (n <= 16384) return f(Shape<512, 32>{});
+  return f(Shape<1024, 32>{});
+}
+// Workgroups for so many rows, and no more than `most` of them, which then take rows in turn.
+template <int TEAM> unsigned groups_for(int64_t rows, int64_t most) {
+  const int64_t each = team_block<TEAM>() / TEAM, want = (rows + each - 1) / each;
+  return (unsigned)(want < most ? want : most);
+}
+
+}  // namespace
+
+extern "C" {
+
+int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask, const float* uniform,
+                 int64_t n_rows, int32_t* actions, float* log_probs, void* stream) {
+  if (!ctx || !how) return PCGRL_E_NULL;
+  const int size = size_of(how->type);
+  if (size == 0 || how->n_classes < 1 || how->n_classes > PCGRL_MAX_CLASSES || n_rows < 0) return PCGRL_E_CONFIG;
+  if (!(how->temperature >= 0.) || !(how->temperature <= 3e38) || !(how->top_p > 0.) || !(how->min_p >= 0. && how->min_p <= 1.) ||
+      how->top_k < 0)
+    return PCGRL_E_CONFIG;
+  if (how->temperature > 0. && how->temperature < 1e-30) return PCGRL_E_CONFIG;
+  if (n_rows == 0) return PCGRL_OK;
+  const bool best = how->temperature == 0.;
+  if (!logits || !actions || (!uniform && !best)) return PCGRL_E_NULL;
+  if (misaligned(logits, size) || misaligned(uniform, 4) || misaligned(actions, 4) || misaligned(log_probs, 4)) return PCGRL_E_CONFIG;
+  if (bad_rows(n_rows, how->logits_stride, how->n_classes)) return PCGRL_E_CONFIG;
+  if (mask && how->mask_stride != 0 && bad_rows(n_rows, how->mask_stride, how->n_classes)) return PCGRL_E_CONFIG;
+  DeviceGuard guard(device_of(ctx));
+  if (!guard.ok) return PCGRL_E_DEVICE;
+  SampleArgs a{};
+  a.logits = logits;
+  a.mask = mask;
+  a.uniform = uniform;
+  a.actions = actions;
+  a.log_probs = log_probs;
+  a.n_rows = n_rows;
+  a.logits_stride = how->logits_stride;
+  a.mask_stride = how->mask_stride;
+  a.n = how->n_classes;
+  a.top_k = how->top_k < how->n_classes ? how->top_k : 0;
+  a.inv_temperature = best ? 0. : 1. / how->temperature;
+  a.slope = 1.44269504088896340736 * a.inv_temperature;
+  a.top_p = how->top_p;
+  a.min_p = how->min_p;
+  const bool cut = a.top_k > 0 || a.top_p < 1. || a.min_p > 0.;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return by_type(how->type, [&](auto type) {
+    return by_classes(a.n, [&](auto shape) {
+      using T = decltype(type);
+      using S = decltype(shape);
+      auto* kernel = best ? &sample_kernel<T, S::kTeam, S::kPer, kSampleBest>
+                     : cut ? &sample_kernel<T, S::kTeam, S::kPer, kSampleCut> : &sample_kernel<T, S::kTeam, S::kPer, kSamplePlain>;
+      hipLaunchKernelGGL(kernel, dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(team_block<S::kTeam>()), 0, st, a);
+      return launched();
+    });
+  });
+}
+
+int pcgrl_step_logits(pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask, const float* uniform,
+                      int32_t* actions, float* log_probs, uint8_t* obs, float* reward, uint8_t* done, void* stream) {
+  if (!ctx || !how) return PCGRL_E_NULL;
+  if (how->n_classes != tiles_in(ctx)) return PCGRL_E_CONFIG;
+  const int rc = pcgrl_sample(ctx, how, logits, mask, uniform, levels_of(ctx), actions, log_probs, stream);
+  return rc == PCGRL_OK ? pcgrl_step(ctx, actions, obs, reward, done, stream) : rc;
+}
+
+int pcgrl_advantages(const pcgrl_ctx* ctx, const float* reward, const uint8_t* done, const void* values, int32_t values_type,
+                     int32_t n_steps, int32_t n_envs, double discount, double trace, float* advantages, float* returns, void* stream) {
+  if (!ctx) return PCGRL_E_NULL;
+  const int size = size_of(values_type);
+  if (size == 0 || n_steps < 0 || n_steps > (1 << 20) || n_envs < 0 || n_envs > (1 << 24)) return PCGRL_E_CONFIG;
+  if (!(discount >= 0. && discount <= 1.) || !(trace >= 0. && trace <= 1.)) return PCGRL_E_CONFIG;
+  if (n_steps == 0 || n_envs == 0) return PCGRL_OK;
+  if (!reward || !done || !values || !advantages) return PCGRL_E_NULL;
+  if (misaligned(reward, 4) || misaligned(values, size) || misaligned(advantages, 4) || misaligned(returns, 4)) return PCGRL_E_CONFIG;
+  const size_t out = (size_t)n_steps * n_envs * 4, in = (size_t)(n_steps + 1) * n_envs * size;
+  for (const float* o : {advantages, returns})
+    if (overlap(o, out, reward, out) || overlap(o, out, done, out / 4) || overlap(o, out, values, in)) return PCGRL_E_CONFIG;
+  if (overlap(advantages, out, returns, out)) return PCGRL_E_CONFIG;
+  DeviceGuard guard(device_of(ctx));
+  if (!guard.ok) return PCGRL_E_DEVICE;
+  const AdvantageArgs a{reward, done, values, advantages, returns, n_steps, n_envs, discount, trace};
+  return by_type(values_type, [&](auto type) {
+    hipLaunchKernelGGL((advantages_kernel<decltype(type)>), dim3((unsigned)((n_envs + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    return launched();
+  });
+}
+
+int64_t pcgrl_policy_loss_workspace(void) { return (int64_t)kLossBlocks * kLossSums * (int64_t)sizeof(double); }
+
+int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
+  if (!ctx || !l) return PCGRL_E_NULL;
+  const int size = size_of(l->type);
+  if (size == 0 || l->n_classes < 1 || l->n_classes > PCGRL_MAX_CLASSES || l->n_rows < 0) return PCGRL_E_CONFIG;
+  if (!(l->temperature >= 1e-30 && l->temperature <= 3e38) || !(l->clip_low >= 0. && l->clip_low <= 1.) || !(l->clip_high >= 0.) ||
+      !std::isfinite(l->clip_high) || !std::isfinite(l->entropy_coef) || !std::isfinite(l->value_coef) || !std::isfinite(l->scale))
+    return PCGRL_E_CONFIG;
+  if (l->stats && !l->workspace) return PCGRL_E_NULL;
+  if (misaligned(l->stats, 4) || misaligned(l->workspace, 8)) return PCGRL_E_CONFIG;
+  if (l->n_rows > 0) {
+    if (!l->logits || !l->actions || !l->advantages || (l->values && !l->returns)) return PCGRL_E_NULL;
+    if (misaligned(l->logits, size) || misaligned(l->actions, 4) || misaligned(l->advantages, 4) || misaligned(l->old_log_probs, 4) ||
+        misaligned(l->values, size) || misaligned(l->returns, 4) || misaligned(l->grad_logits, size) || misaligned(l->grad_values, size) ||
+        misaligned(l->log_probs, 4) || misaligned(l->entropies, 4))
+      return PCGRL_E_CONFIG;
+    if (bad_rows(l->n_rows, l->logits_stride, l->n_classes)) return PCGRL_E_CONFIG;
+    if (l->mask && l->mask_stride != 0 && bad_rows(l->n_rows, l->mask_stride, l->n_classes)) return PCGRL_E_CONFIG;
+    if (l->grad_logits && bad_rows(l->n_rows, l->grad_stride, l->n_classes)) return PCGRL_E_CONFIG;
+    const bool in_place = l->grad_logits == l->logits && (l->n_rows == 1 || l->grad_stride == l->logits_stride);
+    if (!in_place && overlap(l->grad_logits, span(l->n_rows, l->grad_stride, l->n_classes, size), l->logits,
+                             span(l->n_rows, l->logits_stride, l->n_classes, size)))
+      return PCGRL_E_CONFIG;
+  }
+  if (l->n_rows == 0 && !l->stats) return PCGRL_OK;
+  DeviceGuard guard(device_of(ctx));
+  if (!guard.ok) return PCGRL_E_DEVICE;
+  LossArgs a{};
+  a.logits = l->logits;
+  a.mask = l->mask;
+  a.actions = l->actions;
+  a.advantages = l->advantages;
+  a.old = l->old_log_probs;
+  a.values = l->values;
+  a.returns = l->returns;
+  a.grad_logits = l->grad_logits;
+  a.grad_values = l->values ? l->grad_values : nullptr;
+  a.log_probs = l->log_probs;
+  a.entropies = l->entropies;
+  a.partial = l->stats ? static_cast<double*>(l->workspace) : nullptr;
+  a.n_rows = l->n_rows;
+  a.logits_stride = l->logits_stride;
+  a.mask_stride = l->mask_stride;
+  a.grad_stride = l->grad_stride;
+  a.n = l->n_classes;
+  a.inv_temperature = 1. / l->temperature;
+  a.slope = 1.44269504088896340736 * a.inv_temperature;
+  a.low = 1. - l->clip_low;
+  a.high = 1. + l->clip_high;
+  a.entropy_coef = l->entropy_coef;
+  a.value_coef = l->value_coef;
+  a.scale = l->scale;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  unsigned blocks = 0;
+  if (l->n_rows > 0) {
+    const int rc = by_type(l->type, [&](auto type) {
+      return by_classes(a.n, [&](auto shape) {
+        using S = decltype(shape);
+        blocks = groups_for<S::kTeam>(l->n_rows, kLossBlocks);
+        hipLaunchKernelGGL((loss_kernel<decltype(type), S::kTeam, S::kPer>), dim3(blocks), dim3(team_block<S::kTeam>()), 0, st, a);
+        return launched();
+      });
+    });
+    if (rc != PCGRL_OK) return rc;
+  }
+  if (!l->stats) return PCGRL_OK;
+  hipLaunchKernelGGL(loss_sums_kernel, dim3(1), dim3(64 * kLossSums), 0, st, static_cast<const double*>(l->workspace), (int)blocks,
+                     a.entropy_coef, a.value_coef, a.scale, l->stats);
+  return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,146 @@
+"""Host-only checks of the policy's entry points: what they refuse, before any GPU call, and the plain
+statements that the kernels are held to, against hand-computed rows and differences."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import policy_oracle
+from paper_2408_12525_amd import binding
+
+CTX = C.c_void_p(4096)          # (never followed: every call here ends before the context is looked at)
+P, ODD = 1 << 20, (1 << 20) + 1
+OK, NULL, CONFIG = 0, -1, -2
+
+
+def sampling(**more):
+    return binding.PcgrlSampling(**dict(dict(type=3, n_classes=7, logits_stride=7, mask_stride=7, temperature=1.0, top_p=1.0, min_p=0.0, top_k=0), **more))
+
+
+def sample(how=None, ctx=CTX, logits=P, mask=None, uniform=P, n_rows=5, actions=P, log_probs=P, **more):
+    how = sampling(**more) if how is None else how
+    return binding.load().pcgrl_sample(ctx, C.byref(how) if how else None, logits, mask, uniform, n_rows, actions, log_probs, None)
+
+
+@pytest.mark.parametrize("rc,more", [
+    (NULL, dict(ctx=None)), (NULL, dict(how=False)), (NULL, dict(logits=None)), (NULL, dict(uniform=None)), (NULL, dict(actions=None)),
+    (CONFIG, dict(type=0)), (CONFIG, dict(type=4)), (CONFIG, dict(type=-1)), (CONFIG, dict(n_classes=0)), (CONFIG, dict(n_classes=32769, logits_stride=32769)),
+    (CONFIG, dict(n_rows=-1)), (CONFIG, dict(logits_stride=6)), (CONFIG, dict(logits_stride=0)), (CONFIG, dict(logits_stride=-7)),
+    (CONFIG, dict(mask=P, mask_stride=6)), (CONFIG, dict(mask=P, mask_stride=-1)),
+    (CONFIG, dict(temperature=-1.0)), (CONFIG, dict(temperature=math.nan)), (CONFIG, dict(temperature=math.inf)), (CONFIG, dict(temperature=1e-31)),
+    (CONFIG, dict(top_p=0.0)), (CONFIG, dict(top_p=-0.5)), (CONFIG, dict(top_p=math.nan)), (CONFIG, dict(min_p=-0.1)), (CONFIG, dict(min_p=1.1)),
+    (CONFIG, dict(min_p=math.nan)), (CONFIG, dict(top_k=-1)), (CONFIG, dict(logits=P + 2)), (CONFIG, dict(logits=ODD, type=1)), (CONFIG, dict(uniform=P + 2)),
+    (CONFIG, dict(actions=P + 2)), (CONFIG, dict(log_probs=P + 1)),
+    (OK, dict(n_rows=0)), (OK, dict(n_rows=0, logits=None, uniform=None, actions=None, log_probs=None))])
+def test_sample_refuses(rc, more):
+    assert sample(**more) == rc
+
+
+def advantages(ctx=CTX, reward=P, done=2 * P, values=3 * P, code=3, steps=5, envs=3, discount=.99, trace=.95, adv=4 * P, ret=5 * P):
+    return binding.load().pcgrl_advantages(ctx, reward, done, values, code, steps, envs, discount, trace, adv, ret, None)
+
+
+@pytest.mark.parametrize("rc,more", [
+    (NULL, dict(ctx=None)), (NULL, dict(reward=None)), (NULL, dict(done=None)), (NULL, dict(values=None)), (NULL, dict(adv=None)),
+    (CONFIG, dict(code=0)), (CONFIG, dict(code=7)), (CONFIG, dict(steps=-1)), (CONFIG, dict(steps=(1 << 20) + 1)), (CONFIG, dict(envs=-1)),
+    (CONFIG, dict(envs=(1 << 24) + 1)), (CONFIG, dict(discount=-.1)), (CONFIG, dict(discount=1.01)), (CONFIG, dict(discount=math.nan)),
+    (CONFIG, dict(trace=-.1)), (CONFIG, dict(trace=1.5)), (CONFIG, dict(trace=math.nan)), (CONFIG, dict(reward=P + 2)), (CONFIG, dict(values=3 * P + 2)),
+    (CONFIG, dict(values=3 * P + 1, code=2)), (CONFIG, dict(adv=4 * P + 1)), (CONFIG, dict(ret=5 * P + 2)),
+    (CONFIG, dict(adv=P)), (CONFIG, dict(ret=P + 56)), (CONFIG, dict(adv=2 * P - 56)), (CONFIG, dict(adv=2 * P + 12)), (CONFIG, dict(ret=3 * P + 68)), (CONFIG, dict(ret=4 * P + 56)),
+    (OK, dict(steps=0)), (OK, dict(envs=0)), (OK, dict(steps=0, reward=None, done=None, values=None, adv=None))])
+def test_advantages_refuse(rc, more):
+    assert advantages(**more) == rc
+
+
+def policy_loss(ctx=CTX, null=False, **more):
+    d = dict(type=3, n_classes=7, n_rows=5, logits=P, logits_stride=7, mask_stride=7, actions=2 * P, advantages=2 * P, old_log_probs=2 * P, temperature=1.0,
+             clip_low=.2, clip_high=.2, entropy_coef=.01, value_coef=.5, scale=1.0, grad_logits=3 * P, grad_stride=7, stats=4 * P, workspace=5 * P)
+    loss = binding.PcgrlLoss(**dict(d, **more))
+    return binding.load().pcgrl_policy_loss(ctx, None if null else C.byref(loss), None)
+
+
+@pytest.mark.parametrize("rc,more", [
+    (NULL, dict(ctx=None)), (NULL, dict(null=True)), (NULL, dict(logits=None)), (NULL, dict(actions=None)), (NULL, dict(advantages=None)),
+    (NULL, dict(values=P)), (NULL, dict(workspace=None)), (CONFIG, dict(type=0)), (CONFIG, dict(type=9)), (CONFIG, dict(n_classes=0)),
+    (CONFIG, dict(n_classes=40000, logits_stride=40000, grad_stride=40000)), (CONFIG, dict(n_rows=-5)), (CONFIG, dict(logits_stride=5)), (CONFIG, dict(grad_stride=6)),
+    (CONFIG, dict(mask=P, mask_stride=3)), (CONFIG, dict(temperature=0.0)), (CONFIG, dict(temperature=math.nan)), (CONFIG, dict(temperature=-1.0)),
+    (CONFIG, dict(clip_low=-.1)), (CONFIG, dict(clip_low=1.1)), (CONFIG, dict(clip_high=-.1)), (CONFIG, dict(clip_high=math.inf)), (CONFIG, dict(clip_high=math.nan)),
+    (CONFIG, dict(entropy_coef=math.nan)), (CONFIG, dict(value_coef=math.inf)), (CONFIG, dict(scale=math.nan)), (CONFIG, dict(logits=P + 2)), (CONFIG, dict(actions=P + 1)),
+    (CONFIG, dict(advantages=P + 2)), (CONFIG, dict(old_log_probs=P + 2)), (CONFIG, dict(values=P + 2, returns=P)), (CONFIG, dict(values=P, returns=P + 2)),
+    (CONFIG, dict(grad_logits=3 * P + 2)), (CONFIG, dict(grad_values=P + 2)), (CONFIG, dict(log_probs=P + 2)), (CONFIG, dict(entropies=P + 1)), (CONFIG, dict(stats=P + 2)),
+    (CONFIG, dict(workspace=P + 4)), (CONFIG, dict(grad_logits=P, grad_stride=8)), (CONFIG, dict(grad_logits=P + 28)), (CONFIG, dict(grad_logits=P + 136)),
+    (OK, dict(n_rows=0, stats=None, workspace=None, logits=None, grad_logits=None, actions=None, advantages=None))])
+def test_policy_loss_refuses(rc, more):
+    assert policy_loss(**more) == rc
+
+
+def test_step_logits_refuses():
+    L = binding.load()
+    how = sampling()
+    assert L.pcgrl_step_logits(None, C.byref(how), P, None, P, P, None, None, None, None, None) == NULL
+    assert L.pcgrl_step_logits(CTX, None, P, None, P, P, None, None, None, None, None) == NULL
+
+
+def test_workspace_and_structures_are_what_the_header_says(tmp_path):
+    """Sizes and the offsets of the last fields, as the C compiler sees them."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "sizes.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "pcgrl.h"\nint main(void) { printf("%zu %zu %zu %zu %d %d", sizeof(pcgrl_sampling), '
+                   'offsetof(pcgrl_sampling, top_k), sizeof(pcgrl_loss), offsetof(pcgrl_loss, workspace), PCGRL_LOSS_STATS, PCGRL_MAX_CLASSES); return 0; }\n')
+    subprocess.run(["gcc", "-std=c11", "-Wall", "-Werror", "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "sizes")], check=True)
+    got = [int(v) for v in subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [C.sizeof(binding.PcgrlSampling), binding.PcgrlSampling.top_k.offset, C.sizeof(binding.PcgrlLoss), binding.PcgrlLoss.workspace.offset,
+                   binding.LOSS_STATS, 64 * 64 * 8]
+    assert binding.load().pcgrl_policy_loss_workspace() > 0
+
+
+# ---- the plain statements themselves
+
+def test_plain_sampling_by_hand():
+    x = np.log([[4., 2., 1., 1.]])                                # shares 1/2, 1/4, 1/8, 1/8
+    at = lambda u, **how: policy_oracle.sample(x, None, [u], **how)[0][0]  # noqa: E731
+    assert [at(u) for u in (0., .49, .51, .74, .76, .87, .88, 1.)] == [0, 0, 1, 1, 2, 2, 3, 3]
+    assert [at(u, top_k=2) for u in (.6, .7, .99)] == [0, 1, 1]                     # 2/3, 1/3
+    assert [at(u, top_k=3) for u in (.56, .58, .85, .87)] == [0, 1, 1, 2]           # the tie goes to the lower index
+    assert [at(u, top_p=.45) for u in (0., .99)] == [0, 0] and [at(u, top_p=.6) for u in (.6, .7)] == [0, 1]
+    assert [at(u, top_p=.8) for u in (.85, .87, .99)] == [1, 2, 2]                  # 7/8 reach it: the last one is left out
+    assert [at(u, min_p=.4) for u in (.6, .99)] == [0, 1] and at(.99, min_p=.6) == 0 and at(.99, min_p=1.) == 0
+    assert at(.9, top_k=2, top_p=.66) == 0 and at(.9, top_k=2, top_p=.67) == 1      # top_p is of what top_k left
+    assert np.allclose(policy_oracle.sample(x, None, [.6], top_k=2)[1], math.log(.5))
+    assert np.allclose(policy_oracle.sample(x, None, [.51], temperature=.5)[1], math.log(16 / 22))
+    mask = np.array([[0, 1, 0, 1]])
+    assert policy_oracle.sample(x, mask, [.99])[0][0] == 3 and policy_oracle.sample(x, mask * 0, [.5])[0][0] == -1
+    assert policy_oracle.sample(x, mask, [.99], temperature=0)[0][0] == 1
+
+
+def test_plain_advantages_by_hand():
+    r, d, v = [[1.], [2.], [3.]], [[0], [1], [0]], [[10.], [20.], [30.], [40.]]
+    adv, ret = policy_oracle.advantages(r, d, v, .5, .5)
+    assert adv[:, 0].tolist() == [1 + 10 - 10 + .25 * (2 - 20), 2 - 20, 3 + 20 - 30] and ret[:, 0].tolist() == (adv[:, 0] + [10, 20, 30]).tolist()
+
+
+@pytest.mark.parametrize("clipped", [False, True])
+@pytest.mark.parametrize("temperature", [1.0, 0.6])
+def test_plain_gradients_are_the_differences(clipped, temperature):
+    rng = np.random.default_rng(3)
+    n, V = 7, 5
+    x, v = rng.normal(size=(n, V)), rng.normal(size=n)
+    mask = rng.random((n, V)) < .8
+    mask[3] = False
+    actions = np.array([next((j for j in rng.permutation(V) if mask[i, j]), 0) for i in range(n)])
+    actions[5] = -1
+    how = dict(mask=mask, actions=actions, advantages=rng.normal(size=n), old=rng.normal(-1.6, .3, size=n) if clipped else None, returns=rng.normal(size=n),
+               temperature=temperature, entropy_coef=.3, value_coef=.7, scale=.9)
+    f = lambda x, v: policy_oracle.loss(x, values=v, **how)  # noqa: E731
+    got, h = f(x, v), 1e-6
+    for i in range(n):
+        for j in range(V):
+            e = np.zeros_like(x)
+            e[i, j] = h
+            assert abs((f(x + e, v)["loss"] - f(x - e, v)["loss"]) / (2 * h) - got["grad_logits"][i, j]) < 1e-8
+        e = np.zeros(n)
+        e[i] = h
+        assert abs((f(x, v + e)["loss"] - f(x, v - e)["loss"]) / (2 * h) - got["grad_values"][i]) < 1e-8
