@@ -444,6 +444,12 @@ class Pcgrl:
         """Actions [n] int32 drawn from logits [n, classes] with the uniform numbers [n] float32, and their
         log-probabilities [n] float32 under the policy (mask and temperature, without the truncations).
         Rows of logits may lie apart; mask [n, classes] or [classes] uint8 or bool."""
+        got = self._env.sample(logits, uniform, mask, temperature, top_k, top_p, min_p, actions, log_probs)
+        if got != _LOOK:
+            rc, actions, log_probs = got
+            if rc:
+                _check(rc, "pcgrl_sample")
+            return actions, log_probs
         how, x, m, u, n = self._sampling(logits, uniform, mask, None, temperature, top_k, top_p, min_p)
         if actions is None:
             actions = torch.empty((n,), dtype=torch.int32, device=self.device)
@@ -458,6 +464,12 @@ class Pcgrl:
                           actions=None, log_probs=None):
         """pcgrl_sample for every environment and pcgrl_step with the actions drawn; returns what
         pcgrl_sample does."""
+        got = self._env.step_logits(logits, uniform, mask, temperature, top_k, top_p, min_p, actions, log_probs, obs, reward, done)
+        if got != _LOOK:
+            rc, actions, log_probs = got
+            if rc:
+                _check(rc, "pcgrl_step_logits")
+            return actions, log_probs
         how, x, m, u, n = self._sampling(logits, uniform, mask, self.B, temperature, top_k, top_p, min_p)
         if actions is None:
             actions = torch.empty((n,), dtype=torch.int32, device=self.device)
@@ -474,6 +486,12 @@ class Pcgrl:
     def pcgrl_advantages(self, reward, done, values, discount, trace, advantages=None, returns=None):
         """Generalised advantages and returns [T, n] float32 of a rollout: reward [T, n] float32, done [T, n]
         uint8 or bool, values [T + 1, n] float16, bfloat16 or float32."""
+        got = self._env.advantages(reward, done, values, discount, trace, advantages, returns)
+        if got != _LOOK:
+            rc, advantages, returns = got
+            if rc:
+                _check(rc, "pcgrl_advantages")
+            return advantages, returns
         code = self._type(values, "values")
         if not isinstance(reward, torch.Tensor) or reward.dim() != 2:
             raise PcgrlError("reward must be a [steps, environments] tensor")
@@ -497,6 +515,13 @@ class Pcgrl:
         float32), `grad_logits` and, with values, `grad_values`, made here where no tensor is given.  The
         gradients are for logits.backward(grad_logits) or torch.autograd.backward; grad_logits may be
         the logits.  log_probs and entropies [n] float32 are written if given.  scale: default 1 / n."""
+        got = self._env.policy_loss(logits, actions, advantages, old_log_probs, mask, values, returns, temperature, clip_low, clip_high,
+                                    entropy_coef, value_coef, scale, grad_logits, grad_values, log_probs, entropies, stats, workspace)
+        if got != _LOOK:
+            rc, stats, grad_logits, grad_values = got
+            if rc:
+                _check(rc, "pcgrl_policy_loss")
+            return dict(stats=stats, grad_logits=grad_logits, grad_values=grad_values)
         l = PcgrlLoss(type=self._type(logits, "logits"), temperature=temperature, clip_low=clip_low, clip_high=clip_high,
                       entropy_coef=entropy_coef, value_coef=value_coef)
         l.logits, l.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")

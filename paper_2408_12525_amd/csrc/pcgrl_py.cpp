@@ -16,6 +16,8 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
+
 #include "../../include/pcgrl.h"
 
 namespace {
@@ -188,6 +190,197 @@ PyObject* env_get_state(PyObject* self, PyObject*) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the policy's side
+
+int logit_type(const at::Tensor& t) {
+  const c10::ScalarType s = t.scalar_type();
+  return s == at::kHalf ? PCGRL_UNPACK_F16 : s == at::kBFloat16 ? PCGRL_UNPACK_BF16 : s == at::kFloat ? PCGRL_UNPACK_F32 : -1;
+}
+
+// A matrix whose rows are contiguous and may lie apart (one_for_all: or be one and the same); n and V < 0: any size.
+bool rows(PyObject* o, const Env* e, bool one_for_all, int64_t n, int64_t V, void** out, int64_t* stride) {
+  if (!THPVariable_Check(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.get_device() != e->device) return false;
+  const bool one = one_for_all && t.dim() == 1;
+  if (!one && t.dim() != 2) return false;
+  const int64_t tn = one ? n : t.size(0), tV = one ? t.size(0) : t.size(1), across = one ? 0 : t.stride(0), along = one ? t.stride(0) : t.stride(1);
+  if ((n >= 0 && tn != n) || (V >= 0 && tV != V) || (tV > 1 && along != 1)) return false;
+  if (tn > 1 && across < tV && !(one_for_all && across == 0)) return false;
+  *stride = tn > 1 ? across : tV;
+  *out = t.data_ptr();
+  return true;
+}
+bool mask_rows(PyObject* o, const Env* e, int64_t n, int64_t V, void** out, int64_t* stride) {
+  *out = nullptr;
+  *stride = 0;
+  if (o == Py_None) return true;
+  if (!THPVariable_Check(o)) return false;
+  const c10::ScalarType s = THPVariable_Unpack(o).scalar_type();
+  return (s == at::kByte || s == at::kBool) && rows(o, e, true, n, V, out, stride);
+}
+bool number(PyObject* o, double* out) {
+  if (!PyFloat_Check(o) && !PyLong_Check(o)) return false;
+  *out = PyFloat_AsDouble(o);
+  return !(*out == -1. && PyErr_Occurred());
+}
+// An output: the caller's tensor, or a new one where there is none.
+bool output(PyObject* o, const Env* e, c10::ScalarType type, const int64_t* dims, int nd, at::Tensor* t, void** out) {
+  if (o != Py_None) {
+    if (!tensor(o, e, type, -1, dims, nd, out)) return false;
+    *t = THPVariable_Unpack(o);
+    return true;
+  }
+  *t = at::empty(at::IntArrayRef(dims, (size_t)nd), on_device(e, type));
+  *out = t->data_ptr();
+  return true;
+}
+
+struct Draw {
+  pcgrl_sampling how;
+  void *logits, *mask, *uniform, *actions, *log_probs;
+  int64_t n;
+  at::Tensor a, lp;
+};
+// logits, uniform, mask, temperature, top_k, top_p, min_p, actions, log_probs
+bool drawing(PyObject* const* a, const Env* e, int64_t n, Draw* d) {
+  std::memset(&d->how, 0, sizeof(d->how));
+  if (!rows(a[0], e, false, n, -1, &d->logits, &d->how.logits_stride)) return false;
+  const at::Tensor& x = THPVariable_Unpack(a[0]);
+  d->n = x.size(0);
+  d->how.type = logit_type(x);
+  if (d->how.type < 0 || x.size(1) < 1 || x.size(1) > PCGRL_MAX_CLASSES) return false;
+  d->how.n_classes = (int32_t)x.size(1);
+  double k;
+  if (!mask_rows(a[2], e, d->n, x.size(1), &d->mask, &d->how.mask_stride) || !number(a[3], &d->how.temperature) || !PyLong_Check(a[4]) ||
+      !number(a[4], &k) || !(k >= 0. && k <= 2147483647.) || !number(a[5], &d->how.top_p) || !number(a[6], &d->how.min_p))
+    return false;
+  d->how.top_k = (int32_t)k;
+  if (d->how.temperature == 0. ? !optional(a[1], e, at::kFloat, -1, &d->n, 1, &d->uniform) : !tensor(a[1], e, at::kFloat, -1, &d->n, 1, &d->uniform))
+    return false;
+  return output(a[7], e, at::kInt, &d->n, 1, &d->a, &d->actions) && output(a[8], e, at::kFloat, &d->n, 1, &d->lp, &d->log_probs);
+}
+
+PyObject* env_sample(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Env* e = reinterpret_cast<Env*>(self);
+  Draw d;
+  if (n != 9 || !e->ctx || !drawing(a, e, -1, &d)) return look();
+  void* st = stream_of(e);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = pcgrl_sample(e->ctx, &d.how, d.logits, static_cast<const uint8_t*>(d.mask), static_cast<const float*>(d.uniform), d.n,
+                    static_cast<int32_t*>(d.actions), static_cast<float*>(d.log_probs), st);
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(d.a), THPVariable_Wrap(d.lp));
+}
+
+// ... and obs, reward, done
+PyObject* env_step_logits(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Env* e = reinterpret_cast<Env*>(self);
+  Draw d;
+  void *obs, *rew, *done;
+  if (n != 12 || !e->ctx || !optional(a[9], e, at::kByte, -1, e->obs, e->obs_dims, &obs) || !optional(a[10], e, at::kFloat, -1, &e->B, 1, &rew) ||
+      !optional(a[11], e, at::kByte, -1, &e->B, 1, &done) || !drawing(a, e, e->B, &d))
+    return look();
+  void* st = stream_of(e);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = pcgrl_step_logits(e->ctx, &d.how, d.logits, static_cast<const uint8_t*>(d.mask), static_cast<const float*>(d.uniform),
+                         static_cast<int32_t*>(d.actions), static_cast<float*>(d.log_probs), static_cast<uint8_t*>(obs),
+                         static_cast<float*>(rew), static_cast<uint8_t*>(done), st);
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(d.a), THPVariable_Wrap(d.lp));
+}
+
+// advantages(reward, done, values, discount, trace, advantages, returns)
+PyObject* env_advantages(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Env* e = reinterpret_cast<Env*>(self);
+  if (n != 7 || !e->ctx || !THPVariable_Check(a[0]) || !THPVariable_Check(a[1]) || !THPVariable_Check(a[2])) return look();
+  const at::Tensor& r = THPVariable_Unpack(a[0]);
+  if (r.dim() != 2 || r.size(0) > (1 << 20) || r.size(1) > (1 << 24)) return look();
+  const int64_t shape[2] = {r.size(0), r.size(1)}, longer[2] = {shape[0] + 1, shape[1]};
+  const at::Tensor &d = THPVariable_Unpack(a[1]), &v = THPVariable_Unpack(a[2]);
+  const int type = logit_type(v);
+  void *rew, *done, *val, *adv, *ret;
+  double discount, trace;
+  at::Tensor ta, tr;
+  if (type < 0 || !tensor(a[0], e, at::kFloat, -1, shape, 2, &rew) ||
+      !tensor(a[1], e, d.scalar_type() == at::kBool ? at::kBool : at::kByte, -1, shape, 2, &done) || !tensor(a[2], e, v.scalar_type(), -1, longer, 2, &val) ||
+      !number(a[3], &discount) || !number(a[4], &trace) || !output(a[5], e, at::kFloat, shape, 2, &ta, &adv) || !output(a[6], e, at::kFloat, shape, 2, &tr, &ret))
+    return look();
+  void* st = stream_of(e);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = pcgrl_advantages(e->ctx, static_cast<const float*>(rew), static_cast<const uint8_t*>(done), val, type, (int32_t)shape[0], (int32_t)shape[1],
+                        discount, trace, static_cast<float*>(adv), static_cast<float*>(ret), st);
+  Py_END_ALLOW_THREADS
+  return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(ta), THPVariable_Wrap(tr));
+}
+
+// policy_loss(logits, actions, advantages, old_log_probs, mask, values, returns, temperature, clip_low, clip_high, entropy_coef,
+//             value_coef, scale, grad_logits, grad_values, log_probs, entropies, stats, workspace)
+PyObject* env_policy_loss(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Env* e = reinterpret_cast<Env*>(self);
+  if (n != 19 || !e->ctx) return look();
+  pcgrl_loss l;
+  std::memset(&l, 0, sizeof(l));
+  void *x, *m, *act, *adv, *old, *val, *ret, *gx, *gv = nullptr, *lp, *h, *stats, *room;
+  if (!rows(a[0], e, false, -1, -1, &x, &l.logits_stride)) return look();
+  const at::Tensor& t = THPVariable_Unpack(a[0]);
+  const int64_t N = t.size(0), V = t.size(1), dims[2] = {N, V}, n_stats = PCGRL_LOSS_STATS;
+  l.type = logit_type(t);
+  if (l.type < 0 || V < 1 || V > PCGRL_MAX_CLASSES) return look();
+  const c10::ScalarType type = t.scalar_type();
+  at::Tensor tg, tv, ts, tw;
+  if (!tensor(a[1], e, at::kInt, -1, &N, 1, &act) || !tensor(a[2], e, at::kFloat, -1, &N, 1, &adv) || !optional(a[3], e, at::kFloat, -1, &N, 1, &old) ||
+      !mask_rows(a[4], e, N, V, &m, &l.mask_stride) || !optional(a[5], e, type, -1, &N, 1, &val) || !optional(a[6], e, at::kFloat, -1, &N, 1, &ret) ||
+      (val && !ret) || !number(a[7], &l.temperature) || !number(a[8], &l.clip_low) || !number(a[9], &l.clip_high) || !number(a[10], &l.entropy_coef) ||
+      !number(a[11], &l.value_coef))
+    return look();
+  if (a[12] == Py_None) l.scale = 1. / (double)(N > 1 ? N : 1);
+  else if (!number(a[12], &l.scale)) return look();
+  if (!optional(a[15], e, at::kFloat, -1, &N, 1, &lp) || !optional(a[16], e, at::kFloat, -1, &N, 1, &h)) return look();
+  if (a[13] == Py_None) {
+    if (!output(a[13], e, type, dims, 2, &tg, &gx)) return look();
+    l.grad_stride = V;
+  } else {
+    if (!THPVariable_Check(a[13]) || THPVariable_Unpack(a[13]).scalar_type() != type || !rows(a[13], e, false, N, V, &gx, &l.grad_stride)) return look();
+    tg = THPVariable_Unpack(a[13]);
+  }
+  if (val ? !output(a[14], e, type, &N, 1, &tv, &gv) : a[14] != Py_None) return look();
+  const int64_t size = pcgrl_policy_loss_workspace();
+  if (!output(a[17], e, at::kFloat, &n_stats, 1, &ts, &stats)) return look();
+  if (a[18] != Py_None) {
+    if (!THPVariable_Check(a[18]) || THPVariable_Unpack(a[18]).numel() < size) return look();
+    const int64_t all = THPVariable_Unpack(a[18]).numel();
+    if (!tensor(a[18], e, at::kByte, -1, &all, 1, &room)) return look();
+  } else if (!output(a[18], e, at::kByte, &size, 1, &tw, &room)) {
+    return look();
+  }
+  l.n_classes = (int32_t)V;
+  l.n_rows = N;
+  l.logits = x;
+  l.mask = static_cast<const uint8_t*>(m);
+  l.actions = static_cast<const int32_t*>(act);
+  l.advantages = static_cast<const float*>(adv);
+  l.old_log_probs = static_cast<const float*>(old);
+  l.values = val;
+  l.returns = static_cast<const float*>(ret);
+  l.grad_logits = gx;
+  l.grad_values = gv;
+  l.log_probs = static_cast<float*>(lp);
+  l.entropies = static_cast<float*>(h);
+  l.stats = static_cast<float*>(stats);
+  l.workspace = room;
+  void* st = stream_of(e);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = pcgrl_policy_loss(e->ctx, &l, st);
+  Py_END_ALLOW_THREADS
+  PyObject* values = val ? THPVariable_Wrap(tv) : Py_NewRef(Py_None);
+  return Py_BuildValue("(iNNN)", rc, THPVariable_Wrap(ts), THPVariable_Wrap(tg), values);
+}
+
 PyObject* env_close(PyObject* self, PyObject*) {
   reinterpret_cast<Env*>(self)->ctx = nullptr;
   Py_RETURN_NONE;
@@ -244,6 +437,8 @@ PyMethodDef env_methods[] = {
     {"step", fast<env_step>(), METH_FASTCALL, nullptr}, {"rollout", fast<env_rollout>(), METH_FASTCALL, nullptr},
     {"reset", fast<env_reset>(), METH_FASTCALL, nullptr}, {"unpack_obs", fast<env_unpack_obs>(), METH_FASTCALL, nullptr},
     {"set_state", fast<env_set_state>(), METH_FASTCALL, nullptr},
+    {"sample", fast<env_sample>(), METH_FASTCALL, nullptr}, {"step_logits", fast<env_step_logits>(), METH_FASTCALL, nullptr},
+    {"advantages", fast<env_advantages>(), METH_FASTCALL, nullptr}, {"policy_loss", fast<env_policy_loss>(), METH_FASTCALL, nullptr},
     {"metrics", one<env_metrics>(), METH_O, nullptr}, {"exact_diameter", one<env_exact_diameter>(), METH_O, nullptr},
     {"observe", one<env_observe>(), METH_O, nullptr}, {"get_state", env_get_state, METH_NOARGS, nullptr},
     {"close", env_close, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr},

@@ -144,3 +144,48 @@ def test_plain_gradients_are_the_differences(clipped, temperature):
         e = np.zeros(n)
         e[i] = h
         assert abs((f(x, v + e)["loss"] - f(x, v - e)["loss"]) / (2 * h) - got["grad_values"][i]) < 1e-8
+
+
+# ---- the compiled call path
+
+def test_doubtful_arguments_are_left_to_the_python_checks():
+    """Tensors that are not on the device, missing arguments, numbers that are none, and a closed environment (no GPU is
+    touched)."""
+    import torch
+    py = binding._load_py()
+    env = py.Env(1, 0, 4, 16, 16, (3, 2, 31, 31), (3, 2, 31, 31))   # (the handle is never followed)
+    x, u = torch.zeros((3, 2)), torch.zeros(3)
+    calls = lambda e: [e.sample(x, u, None, 1.0, 0, 1.0, 0.0, None, None), e.sample(None, u, None, 1.0, 0, 1.0, 0.0, None, None), e.sample(x), e.sample(x, u, None, "1", 0, 1.0, 0.0, None, None),  # noqa: E731
+                       e.step_logits(x, u, None, 1.0, 0, 1.0, 0.0, None, None, None, None, None), e.step_logits(x, u), e.advantages(x, x, x, .9, .9, None, None), e.advantages(None, x, x, .9, .9, None, None),
+                       e.advantages(x, x), e.policy_loss(x, u, u), e.policy_loss(*[x, u, u] + [None] * 16), e.policy_loss(*[None] * 19)]
+    assert set(calls(env)) == {py.LOOK}
+    env.close()
+    assert set(calls(env)) == {py.LOOK}
+
+
+WRAPPED = """
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+from paper_2408_12525_amd import binding
+py = binding._load_py()
+env = py.Env(1, 0, 4, 16, 16, (3, 2, 31, 31), (3, 2, 31, 31))   # (the handle is never followed)
+asked = []
+def inside(x, u, a, d, v):
+    asked.extend([env.sample(x, u, None, 1.0, 0, 1.0, 0.0, a, u), env.step_logits(x, u, None, 1.0, 0, 1.0, 0.0, a, u, None, None, None),
+                  env.advantages(x, d, v, .9, .9, x, x), env.policy_loss(x, a, u, u, None, None, None, 1.0, .2, .2, 0.0, .5, 1.0, x, None, None, None, None, None)])
+    return u
+with FakeTensorMode():
+    e = lambda t, *s: torch.empty((2,) + s, dtype=t, device="cuda:0")
+    torch.vmap(inside)(e(torch.float32, 3, 2), e(torch.float32, 3), e(torch.int32, 3), e(torch.uint8, 3, 2), e(torch.float32, 4, 2))
+assert asked == [py.LOOK] * 4, asked
+print("asked")
+"""
+
+
+def test_the_call_path_outlives_tensors_without_storage():
+    """What torch throws in an argument check ends neither the call nor the process."""
+    import os
+    import subprocess
+    import sys
+    res = subprocess.run([sys.executable, "-c", WRAPPED], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True)
+    assert res.returncode == 0 and res.stdout.split() == ["asked"], res.stderr[-2000:]
