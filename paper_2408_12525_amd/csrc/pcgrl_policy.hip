@@ -51,6 +51,36 @@ template <int TEAM> unsigned groups_for(int64_t rows, int64_t most) {
   return (unsigned)(want < most ? want : most);
 }
 
+// How advantages are shared out over workgroups: sets the environments and steps of one, and returns the groups
+// that the steps are cut into.  Measured, us:
+//   Few environments: as many threads along the steps as take all of them at once, 64 steps of 64 environments
+//   with 4 / 16 / 32 environments a workgroup 4.4 / 3.8 / 3.5, 2000 of 64 with 1 / 4 / 8 9.9 / 12.0 / 20.2.
+//   Where that takes several turns of 2.5 us the steps are cut into groups, at the price of two more launches and
+//   of reading the inputs twice: 10 000 steps of 16 10.5 against 32, of 1 14.9 against 23.4, but 3000 of 1 13.2 against
+//   9.5, 1000 of 4096 21.5 against 23.6 and 300 of 4096 12.6 against 10.3.
+//   Many: rows of a workgroup as wide as leave enough workgroups, 300 steps of 8000 with 16 / 32 / 64
+//   environments 16.2 / 14.0 / 15.8, 128 of 65 536 with 32 / 64 / 256 27.4 / 21.8 / 27.7, 32 of 262 145 with 64 / 256 31 / 24.
+int share_steps(AdvantageArgs* a) {
+  const int n = a->n_envs, T = a->n_steps;
+  const bool cut = n < 4096 && T > (n <= 64 ? 4096 : 2048);
+  int fit = 0, lg = n >= 131072 ? 8 : n >= 32768 ? 6 : n >= 8000 ? 5 : n >= 4096 ? 4 : 0;
+  while (fit < 6 && (T << (fit + 1)) <= kAdvantageThreads * kAdvantageSteps) ++fit;
+  if (cut) lg = n > 2048 ? 6 : n > 512 ? 5 : 4;
+  else if (fit > lg) lg = fit;
+  while (lg > 0 && (1 << (lg - 1)) >= n) --lg;
+  a->envs_log2 = lg;
+  if (!cut) return 1;
+  const int at_once = (kAdvantageThreads >> lg) * kAdvantageSteps;
+  const int across = (n + (1 << lg) - 1) >> lg, pieces = (T + at_once - 1) / at_once, room = kAdvantageEach * (kAdvantageThreads >> lg);
+  int groups = 1600 / across;
+  groups = groups < pieces ? groups : pieces;
+  groups = groups < room ? groups : room;
+  if (groups < 2) return 1;
+  const int each = (pieces + groups - 1) / groups;
+  a->group = each * at_once;
+  return (pieces + each - 1) / each;
+}
+
 }  // namespace
 
 extern "C" {
@@ -124,9 +154,19 @@ int pcgrl_advantages(const pcgrl_ctx* ctx, const float* reward, const uint8_t* d
   if (overlap(advantages, out, returns, out)) return PCGRL_E_CONFIG;
   DeviceGuard guard(device_of(ctx));
   if (!guard.ok) return PCGRL_E_DEVICE;
-  const AdvantageArgs a{reward, done, values, advantages, returns, n_steps, n_envs, discount, trace};
+  AdvantageArgs a{reward, done, values, advantages, returns, n_steps, n_envs, 0, n_steps, discount, discount * trace};
+  const int groups = share_steps(&a);
+  const dim3 block(kAdvantageThreads), grid((unsigned)((n_envs + (1 << a.envs_log2) - 1) >> a.envs_log2), (unsigned)groups);
+  hipStream_t st = static_cast<hipStream_t>(stream);
   return by_type(values_type, [&](auto type) {
-    hipLaunchKernelGGL((advantages_kernel<decltype(type)>), dim3((unsigned)((n_envs + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    using T = decltype(type);
+    if (groups == 1) {
+      hipLaunchKernelGGL((advantages_kernel<T, kAdvantageAll>), grid, block, 0, st, a);
+      return launched();
+    }
+    hipLaunchKernelGGL((advantages_kernel<T, kAdvantageSum>), dim3(grid.x, grid.y - 1), block, 0, st, a);
+    hipLaunchKernelGGL(advantages_join_kernel, dim3(grid.x), block, 0, st, a, groups);
+    hipLaunchKernelGGL((advantages_kernel<T, kAdvantageApply>), grid, block, 0, st, a);
     return launched();
   });
 }

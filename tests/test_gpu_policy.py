@@ -357,7 +357,7 @@ def test_no_rows(env):
 # ---- advantages
 
 @pytest.mark.parametrize("T,n", [(1, 1), (2, 1), (1, 300), (3, 5), (7, 64), (8, 65), (9, 63), (33, 17), (64, 16), (100, 1000), (257, 31), (1000, 3), (4096, 2), (513, 257), (31, 4100), (40, 20001),
-                                 (10001, 1), (5000, 33)])
+                                 (10001, 1), (5000, 33), (4097, 64), (2049, 65), (2600, 700), (2100, 2100), (30000, 5), (64, 131073), (20, 32768), (1, 1), (130000, 1)])
 def test_advantages(env, T, n):
     rng = np.random.default_rng(T * 1000 + n)
     for k, dtype in enumerate(TYPES.values()):
