@@ -40,7 +40,9 @@ template <typename F> int by_classes(int n, F&& f) {
   if (n <= 8) return f(Shape<1, 8>{});
   if (n <= 64) return f(Shape<8, 8>{});
   if (n <= 512) return f(Shape<64, 8>{});
+  if (n <= 1024) return f(Shape<64, 16>{});
   if (n <= 2048) return f(Shape<256, 8>{});
+  if (n <= 4096) return f(Shape<256, 16>{});
   if (n <= 8192) return f(Shape<256, 32>{});
   if (n <= 16384) return f(Shape<512, 32>{});
   return f(Shape<1024, 32>{});
@@ -114,7 +116,8 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
   a.n = how->n_classes;
   a.top_k = how->top_k < how->n_classes ? how->top_k : 0;
   a.inv_temperature = best ? 0. : 1. / how->temperature;
-  a.slope = 1.44269504088896340736 * a.inv_temperature;
+  a.slope = 64. * 1.44269504088896340736 * a.inv_temperature;
+  a.reach = (float)(40. * 0.69314718055994530942 * how->temperature);
   a.top_p = how->top_p;
   a.min_p = how->min_p;
   const bool cut = a.top_k > 0 || a.top_p < 1. || a.min_p > 0.;
@@ -218,7 +221,7 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
   a.grad_stride = l->grad_stride;
   a.n = l->n_classes;
   a.inv_temperature = 1. / l->temperature;
-  a.slope = 1.44269504088896340736 * a.inv_temperature;
+  a.slope = 64. * 1.44269504088896340736 * a.inv_temperature;
   a.low = 1. - l->clip_low;
   a.high = 1. + l->clip_high;
   a.entropy_coef = l->entropy_coef;

@@ -10,6 +10,8 @@
 
 #include <cstdint>
 
+#include "../../include/pcgrl.h"
+
 namespace pcgrl {
 
 struct F32 {
@@ -28,17 +30,13 @@ struct BF16 {
   using raw = uint16_t;
   static constexpr int kKeyShift = 16;
   static __device__ float load(raw r) { return __uint_as_float((uint32_t)r << 16); }
-  static __device__ raw store(float f) {  // to nearest, ties to even; a NaN stays one
-    const uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (raw)((u >> 16) | 0x40u);
-    return (raw)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-  }
+  static __device__ raw store(float f) { return __builtin_bit_cast(raw, (__bf16)f); }  // (one instruction, to nearest even)
 };
 
 constexpr float kNone = -__builtin_huge_valf();  // the logit of a class that may not be chosen
 
 // 2^z for z <= 0 (0 below -1000, NaN for NaN), to about 2^-52: the powers of f in [-1/2, 1/2] with ln(2)^k / k!.
-__device__ inline double pow2(double z) {
+__device__ __forceinline__ double pow2(double z) {
   z = z < -1000. ? -1000. : z;
   const double n = __builtin_rint(z), f = z - n;
   double p = 2.5678435993488196e-11;   // ln(2)^12 / 12!
@@ -58,21 +56,78 @@ __device__ inline double pow2(double z) {
 }
 
 // Floats in their order as unsigned integers.
-__device__ inline uint32_t key_of(float x) {
+__device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t u = __float_as_uint(x);
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
+// Lets the compiler forget what it has computed from the classes of a thread: what it would keep from one pass over them to
+// the next takes more registers than there are.
+template <int TEAM, int PER> __device__ __forceinline__ void forget_classes(float (&x)[PER], int& rank) {
+  if constexpr (TEAM >= 64) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) asm volatile("" : "+v"(x[j]));
+    asm volatile("" : "+v"(rank));
+  }
+}
+
+// Values of other lanes.
+template <int CTRL> __device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+template <int CTRL> __device__ __forceinline__ float moved(float v) { return __int_as_float(moved<CTRL>(__float_as_int(v))); }
+template <int CTRL> __device__ __forceinline__ double moved(double v) { return __hiloint2double(moved<CTRL>(__double2hiint(v)), moved<CTRL>(__double2loint(v))); }
+__device__ __forceinline__ int of_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float of_lane(float v, int lane) { return __int_as_float(of_lane(__float_as_int(v), lane)); }
+__device__ __forceinline__ double of_lane(double v, int lane) { return __hiloint2double(of_lane(__double2hiint(v), lane), of_lane(__double2loint(v), lane)); }
+
+// op over the first LANES lanes of every LANES, in all of them.
+template <int LANES, typename V, typename Op> __device__ __forceinline__ V over_lanes(V v, Op op) {
+  static_assert(LANES == 1 || LANES == 8 || LANES == 64, "");
+  if constexpr (LANES >= 8) {
+    v = op(v, moved<0xB1>(v));   // the other of a pair
+    v = op(v, moved<0x4E>(v));   // the other pair of four
+    v = op(v, moved<0x141>(v));  // the other four of eight
+  }
+  if constexpr (LANES == 64) {
+    v = op(v, moved<0x140>(v));  // the other eight of sixteen
+    v = op(op(of_lane(v, 0), of_lane(v, 16)), op(of_lane(v, 32), of_lane(v, 48)));
+  }
+  return v;
+}
+// Sum over the lanes before and including this one, of every LANES.
+template <int LANES, typename V> __device__ __forceinline__ V sum_until(V v) {
+  const int lane = threadIdx.x & (LANES - 1);
+#pragma unroll
+  for (int d = 1; d < LANES; d <<= 1) {
+    const V o = __shfl_up(v, d, LANES);
+    v += lane >= d ? o : (V)0;
+  }
+  return v;
+}
+
 // What the threads of a team know together.
 template <int TEAM> struct Team {
-  static constexpr int kWaves = TEAM > 64 ? TEAM / 64 : 1;
+  static constexpr int kWaves = TEAM > 64 ? TEAM / 64 : 1, kLanes = TEAM < 64 ? TEAM : 64;
   double* room;  // LDS: two sets of a double for each wavefront, used in turn, so that one barrier a sum is enough
   int turn = 0;
   __device__ static int rank() { return TEAM == 1 ? 0 : (int)(threadIdx.x & (TEAM - 1)); }
-  template <typename V, typename Op> __device__ V all(V v, Op op) {
-    constexpr int kIn = TEAM < 64 ? TEAM : 64;
-#pragma unroll
-    for (int d = 1; d < kIn; d <<= 1) v = op(v, __shfl_xor(v, d));
+  // (what follows from it is computed for each row: kept from row to row it takes more registers than there are)
+  __device__ __forceinline__ static int rank_anew() {
+    int r = rank();
+    asm volatile("" : "+v"(r));
+    return r;
+  }
+  // Orders what a team has written to LDS before what it reads afterwards.
+  __device__ static void sync() {
+    if constexpr (TEAM > 64) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  }
+  template <typename V, typename Op> __device__ __forceinline__ V all(V v, Op op) {
+    v = over_lanes<kLanes>(v, op);
     if constexpr (TEAM > 64) {
       V* at = reinterpret_cast<V*>(room + turn * kWaves);
       turn ^= 1;
@@ -90,6 +145,24 @@ template <int TEAM> struct Team {
   __device__ int sum(int v) {
     return all(v, [](int a, int b) { return a + b; });
   }
+  // The sum, and what of it is in the wavefronts before this one and in this one.
+  __device__ double sum(double v, double& before, double& here) {
+    here = over_lanes<kLanes>(v, [](double a, double b) { return a + b; });
+    before = 0.;
+    if constexpr (TEAM > 64) {
+      double *at = room + turn * kWaves, all = 0.;
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = here;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        before = i == (int)(threadIdx.x >> 6) ? all : before;
+        all += at[i];
+      }
+      return all;
+    }
+    return here;
+  }
   __device__ int least(int v) {
     return all(v, [](int a, int b) { return a < b ? a : b; });
   }
@@ -98,55 +171,87 @@ template <int TEAM> struct Team {
   }
 };
 
+// Powers of two by a table of 2^(i / 64), 64 doubles in LDS, times `unit`: power() is unit * 2^(z / 64) to 2^-44, with four terms
+// of the series of what is left of z, 18 instructions.
+__device__ __forceinline__ void fill_powers(double* table, double unit) {
+  if (threadIdx.x < 64) table[threadIdx.x] = unit * 2. * pow2((double)threadIdx.x / 64. - 1.);
+  __syncthreads();
+}
+__device__ __forceinline__ double power(const double* table, double z) {
+  z = __builtin_fmax(z, -64000.);
+  const double t = z + 0x1.8p52, r = z - (t - 0x1.8p52);  // the nearest whole number, in the low word of t
+  const int n = __double2loint(t);
+  double q = 5.732851688640402e-10;                       // (ln(2) / 64)^4 / 4!
+  q = __builtin_fma(q, r, 2.1173137155464774e-07);        // 3
+  q = __builtin_fma(q, r, 5.864904955056169e-05);         // 2
+  q = __builtin_fma(q, r, 0.010830424696249145) * r;      // 1
+  const double of = table[n & 63], v = __builtin_fma(of, q, of);
+  return __hiloint2double(__double2hiint(v) + ((n & ~63) << 14), __double2loint(v));
+}
+
 // The classes of a thread: pieces of VEC neighbouring ones; each wavefront of a team has one stretch of the
-// row, in which its lanes' pieces lie side by side, so that running sums go from wavefront to wavefront.
+// row, in which its lanes' pieces lie side by side, so that running sums go from wavefront to wavefront.  A piece is read at
+// once, whatever its alignment; the one that the row ends in is read as the last VEC classes, of which
+// those of the piece before are left out.
 template <typename T, int TEAM, int PER> struct Row {
   static constexpr int VEC = PER < 16 / (int)sizeof(typename T::raw) ? PER : 16 / (int)sizeof(typename T::raw);
   static constexpr int PIECES = PER / VEC;
   static constexpr int LANES = TEAM < 64 ? TEAM : 64;
-  // first class of piece c
-  static __device__ int at(int c) {
-    const int r = Team<TEAM>::rank();
+  // first class of piece c of the team's thread r
+  static __device__ __forceinline__ int begin(int r, int c) {
     return (r / LANES) * (LANES * PER) + (c * LANES + r % LANES) * VEC;
   }
-  // Logits of the classes that may be chosen, kNone for the others.  (+0 for -0: they are equal.)
-  static __device__ void load(const typename T::raw* row, const uint8_t* mask, int n, float (&x)[PER]) {
+  // the class of element e of piece c
+  static __device__ __forceinline__ int at(int r, int c, int e, int n) {
+    const int first = begin(r, c);
+    return (TEAM > 1 && first > n - VEC ? n - VEC : first) + e;
+  }
+  // Logits of the classes that may be chosen, kNone for the others.
+  static __device__ __forceinline__ void load(const typename T::raw* row, const uint8_t* mask, int r, int n, float (&x)[PER]) {
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) {
-      const int at0 = at(c);
+      const int first = begin(r, c), from = TEAM > 1 && first > n - VEC ? n - VEC : first;
       typename T::raw v[VEC];
       uint8_t m[VEC];
-      if (at0 + VEC <= n) {
-        __builtin_memcpy(v, row + at0, sizeof(v));
-        if (mask) __builtin_memcpy(m, mask + at0, sizeof(m));
+      if (TEAM > 1 ? first < n : first + VEC <= n) {
+        __builtin_memcpy(v, row + from, sizeof(v));
+        if (mask) __builtin_memcpy(m, mask + from, sizeof(m));
+        else __builtin_memset(m, 1, sizeof(m));
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[c * VEC + e] = mask && m[e] == 0 ? kNone : T::load(v[e]) + 0.f;
+        for (int e = 0; e < VEC; ++e) x[c * VEC + e] = m[e] == 0 || (TEAM > 1 && from + e < first) ? kNone : T::load(v[e]);
       } else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const int i = at0 + e;
-          x[c * VEC + e] = i < n && (!mask || mask[i] != 0) ? T::load(row[i]) + 0.f : kNone;
+          const int i = first + e;
+          x[c * VEC + e] = TEAM == 1 && i < n && (!mask || mask[i] != 0) ? T::load(row[i]) : kNone;
         }
       }
     }
   }
-  static __device__ void store(typename T::raw* row, int n, const float (&g)[PER]) {
+  static __device__ __forceinline__ void store(typename T::raw* row, int r, int n, int c, const float (&g)[VEC]) {
+    const int first = begin(r, c), from = TEAM > 1 && first > n - VEC ? n - VEC : first;
+    typename T::raw v[VEC];
 #pragma unroll
-    for (int c = 0; c < PIECES; ++c) {
-      const int at0 = at(c);
-      if (at0 + VEC <= n) {
-        typename T::raw v[VEC];
+    for (int e = 0; e < VEC; ++e) v[e] = T::store(g[e]);
+    if (first + VEC <= n) {
+      __builtin_memcpy(row + first, v, sizeof(v));
+    } else if (first < n) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = T::store(g[c * VEC + e]);
-        __builtin_memcpy(row + at0, v, sizeof(v));
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (at0 + e < n) row[at0 + e] = T::store(g[c * VEC + e]);
-      }
+      for (int e = 0; e < VEC; ++e)
+        if (from + e >= first && from + e < n) row[from + e] = v[e];
     }
   }
 };
+
+// Keeps the compiler from taking more than four classes of a thread through a loop at once, by having the sums over them
+// done: what more take in registers costs more than it hides (28 672 classes a row went through scratch memory).
+template <typename V> __device__ __forceinline__ void done(V& v) { asm volatile("" : "+v"(v)); }
+template <typename... V> __device__ __forceinline__ void part_end(int j, V&... sums) {
+  if (j % 4 == 3) {
+    (done(sums), ...);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 template <int TEAM> constexpr int team_block() { return TEAM > 64 ? TEAM : 256; }
 
@@ -160,7 +265,8 @@ struct SampleArgs {
   float* log_probs;
   int64_t n_rows, logits_stride, mask_stride;
   int32_t n, top_k;     // (top_k: 0 or 1..n-1)
-  double slope;         // log2(e) / temperature
+  double slope;         // 64 * log2(e) / temperature
+  float reach;          // below the largest logit by more than this there are no weights
   double inv_temperature, top_p, min_p;
 };
 
@@ -176,30 +282,413 @@ template <int CLASSES> constexpr double weight_unit() {
   return (double)(1ll << bits);
 }
 
-template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(team_block<TEAM>()) void sample_kernel(SampleArgs a) {
+// The last of the classes that top_k and top_p keep, in the order of falling logits and rising indices.
+template <typename T, int TEAM, int PER> struct Held;
+struct Cutoff {
+  uint32_t key;
+  int index;
+};
+
+// LDS of a team that looks for it: weights and numbers of classes in bins of falling logits, and the classes of one bin.
+template <int TEAM> struct CutRoom {
+  static constexpr int kBins = TEAM == 64 ? 512 : 2048, kList = TEAM == 64 ? 128 : 512;
+  double mass[kBins];
+  double weight[kList];
+  int count[kBins];
+  uint32_t key[kList];
+  int index[kList];
+  double wave_mass[TEAM / 64];
+  int wave_count[TEAM / 64];
+  double mass_before, mass_until;
+  int bin, count_before, listed;
+  Cutoff found;
+  __device__ __forceinline__ void clear(int rank) {
+    for (int b = rank; b < kBins; b += TEAM) {
+      mass[b] = 0.;
+      count[b] = 0;
+    }
+  }
+  // of a class so far below the largest logit (a NaN, of 0 times infinity, goes to the last bin, with all others)
+  static __device__ int bin_of(float below, float scale) { return (int)__builtin_fminf(below * scale, (float)(kBins - 1)); }
+};
+template <> struct CutRoom<8> {};
+template <> struct CutRoom<1> {};
+
+// The classes of one thread.  Their weights are not held but computed again where they are needed: with them in registers a
+// workgroup of 1024 threads would have no room for its row.
+template <typename T, int TEAM, int PER> struct Held {
   using R = Row<T, TEAM, PER>;
-  __shared__ double room[TEAM > 64 ? 2 * TEAM / 64 : 1];
-  __shared__ double wave_sums[TEAM > 64 ? TEAM / 64 : 1];
-  __shared__ int found;
-  Team<TEAM> team{room};
-  constexpr int kTeams = team_block<TEAM>() / TEAM;
-  constexpr double kUnit = weight_unit<TEAM * PER>();
-  for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
-    float x[PER];
-    R::load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, a.n, x);
-    float top = kNone;
-    int odd = 0;  // a NaN or +infinity
+  float x[PER];
+  int rank, n;
+  float top;
+  double slope;
+  const double* table;
+  // (the two zeros are equal)
+  __device__ __forceinline__ uint32_t key(int j) const { return key_of(x[j] + 0.f) >> T::kKeyShift; }
+  __device__ __forceinline__ double weight(int j) const { return __builtin_rint(power(table, ((double)x[j] - (double)top) * slope)); }
+  __device__ __forceinline__ int at(int j) const { return R::at(rank, j / R::VEC, j % R::VEC, n); }
+  // One of the pieces.
+  template <int VEC> __device__ __forceinline__ Held<T, TEAM, VEC> piece(int which) const {
+    Held<T, TEAM, VEC> p;
+    p.rank = rank;
+    p.n = n;
+    p.top = top;
+    p.slope = slope;
+    p.table = table;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float v = x[e];
+      asm("" : "+v"(v));
+#pragma unroll
+      for (int c = 1; c < PER / VEC; ++c) {
+        float o = x[c * VEC + e];
+        asm("" : "+v"(o));
+        v = which == c ? o : v;
+      }
+      p.x[e] = v;
+    }
+    return p;
+  }
+  __device__ __forceinline__ void forget() { forget_classes<TEAM, PER>(x, rank); }
+};
+template <typename T> __device__ __forceinline__ uint32_t no_key() { return key_of(kNone) >> T::kKeyShift; }
+
+// In the order of the classes, the one at which the running sum of `value` first exceeds `target`: calls `found` with it in the
+// lane that holds it.  `piece` has the sums of this thread's pieces, `before` that of the wavefronts before this
+// one, `here` that of this one.  All sums are exact, so that there is one such class if 0 <= target < the sum of all.
+template <typename T, int TEAM, int PER, typename V, typename F>
+__device__ __forceinline__ void find_class(const Held<T, TEAM, PER>& h, const double (&piece)[Row<T, TEAM, PER>::PIECES], double before, double here, double target,
+                                           V value, F found) {
+  using R = Row<T, TEAM, PER>;
+  if (R::LANES == 64 && !(before <= target && target < before + here)) return;
+  // the piece, and its classes
+  double sum = 0., until = 0.;
+  int which = 0;
+#pragma unroll
+  for (int c = 0; c < R::PIECES; ++c) {
+    const double all = over_lanes<R::LANES>(piece[c], [](double a, double b) { return a + b; });
+    const bool it = c == 0 || !(target < before);
+    which = it ? c : which;
+    sum = it ? piece[c] : sum;
+    until = it ? before : until;
+    before += all;
+  }
+  Held<T, TEAM, R::VEC> in = h.template piece<R::VEC>(which);
+  until += sum_until<R::LANES>(sum);
+  double run = until - sum;
+  if (run <= target && target < until) {
+    int at = -1;
+    float logit = 0.f;
+#pragma unroll
+    for (int e = 0; e < R::VEC; ++e) {
+      const int index = R::at(h.rank, which, e, h.n);
+      run += value(in, e, index);
+      float x = in.x[e];
+      asm("" : "+v"(x));  // (else it becomes an address chosen among the classes, and they go to memory)
+      const bool it = at < 0 && run > target;
+      at = it ? index : at;
+      logit = it ? x : logit;
+    }
+    found(at, logit);
+  }
+}
+
+// A lane that holds a whole row: each class against every other one.
+template <typename T, int PER> __device__ __forceinline__ Cutoff cut_lane(const Held<T, 1, PER>& h, const SampleArgs& a, const double (&w)[PER]) {
+  int before[PER];
+  double mass[PER], whole = 0.;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    before[j] = 0;
+    mass[j] = 0.;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (i == j) continue;
+      const bool first = h.x[i] > h.x[j] || (i < j && h.x[i] == h.x[j]);
+      before[j] += first;
+      mass[j] += first ? w[i] : 0.;
+    }
+  }
+  const int k = a.top_k > 0 ? a.top_k : PER;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) whole += before[j] < k ? w[j] : 0.;
+  const double share = a.top_p < 1. ? a.top_p * whole : __builtin_huge_val();
+  Cutoff cut{0, 0x7fffffff};
+  int most = -1;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const bool last = before[j] < k && mass[j] < share && before[j] > most;
+    most = last ? before[j] : most;
+    cut.key = last ? h.key(j) : cut.key;
+    cut.index = last ? j : cut.index;
+  }
+  return cut;
+}
+
+// The last of the first `ties` classes of the key `key`, by index.
+template <typename T, int TEAM, int PER> __device__ __forceinline__ Cutoff cut_ties(Held<T, TEAM, PER>& h, Team<TEAM>& team, uint32_t key, int ties, Cutoff* shared) {
+  using R = Row<T, TEAM, PER>;
+  double piece[R::PIECES], mine = 0., before, here;
+  h.forget();
+#pragma unroll
+  for (int c = 0; c < R::PIECES; ++c) {
+    piece[c] = 0.;
+#pragma unroll
+    for (int e = 0; e < R::VEC; ++e) piece[c] += h.key(c * R::VEC + e) == key ? 1. : 0.;
+    mine += piece[c];
+  }
+  Cutoff cut{key, 0x7fffffff};
+  if (team.sum(mine, before, here) > (double)ties) {
+    int last = 0x7fffffff;
+    find_class(h, piece, before, here, (double)(ties - 1), [&](const Held<T, TEAM, R::VEC>& in, int e, int) { return in.key(e) == key ? 1. : 0.; },
+               [&](int at, float) { last = at; });
+    if constexpr (TEAM > 64) {
+      if (last != 0x7fffffff) shared->index = last;
+      team.sync();
+      last = shared->index;
+      team.sync();
+    } else {
+      last = team.least(last);
+    }
+    cut.index = last;
+  }
+  return cut;
+}
+
+// By halving the range of keys: a sum over the team for each bit.
+template <typename T, int TEAM, int PER>
+__device__ __forceinline__ Cutoff cut_by_halves(Held<T, TEAM, PER>& h, Team<TEAM>& team, const SampleArgs& a, double whole, Cutoff* shared) {
+  constexpr int kBits = 32 - T::kKeyShift;
+  auto count_from = [&](uint32_t k) {
+    int c = 0;
+    h.forget();
+#pragma unroll
+    for (int j = 0; j < PER; ++j) c += h.key(j) >= k;
+    return team.sum(c);
+  };
+  auto sum_from = [&](uint32_t k) {
+    double s = 0.;
+    h.forget();
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      top = x[j] > top ? x[j] : top;
-      odd |= !(x[j] < __builtin_huge_valf());
+      s += h.key(j) >= k ? h.weight(j) : 0.;
+      part_end(j, s);
     }
-    top = team.most(top);
-    odd = team.sum(odd);
-    if (odd != 0 || top == kNone) {
-      if (team.rank() == 0) {
+    return team.sum(s);
+  };
+  auto weight_at = [&](uint32_t k) {  // of a class with this key
+    double v = 0.;
+    h.forget();
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      v = h.key(j) == k ? h.weight(j) : v;
+      part_end(j, v);
+    }
+    return team.all(v, [](double a, double b) { return a > b ? a : b; });
+  };
+  uint32_t edge = 0;
+  int ties = 0x7fffffff;  // classes of the key `edge` that are kept
+  if (a.top_k > 0 && count_from(no_key<T>() + 1) > a.top_k) {
+#pragma unroll 1
+    for (int b = kBits - 1; b >= 0; --b) {
+      const uint32_t k = edge | (1u << b);
+      if (count_from(k) >= a.top_k) edge = k;
+    }
+    ties = a.top_k - count_from(edge + 1);
+    whole = sum_from(edge + 1) + ties * weight_at(edge);
+  }
+  if (a.top_p < 1.) {
+    const double share = a.top_p * whole;
+    uint32_t low = 0;
+#pragma unroll 1
+    for (int b = kBits - 1; b >= 0; --b) {
+      const uint32_t k = low | (1u << b);
+      if (sum_from(k) >= share) low = k;
+    }
+    // (not below `edge`: all of its classes together reach the share)
+    const double above = sum_from(low + 1), one = weight_at(low);
+    const int more = one > 0. ? (int)__builtin_fmin(__builtin_ceil((share - above) / one), (double)PCGRL_MAX_CLASSES) : 1;
+    ties = low == edge && ties < more ? ties : more;
+    edge = low;
+  }
+  return cut_ties<T, TEAM, PER>(h, team, edge, ties, shared);
+}
+
+// By bins: the weights (for top_k the numbers) of a row's classes are added up in LDS in bins of equal width from the
+// largest logit down to the smallest one, or to where weights vanish; the bin in which the sum from the
+// top reaches what is looked for is listed, and each of its few classes is ranked against the others.  Three passes over the
+// row in registers, whatever the types.  A bin with more classes than the list holds is binned again by itself, unless they are
+// all equal: then they are counted off by index.
+template <typename T, int TEAM, int PER>
+__device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double whole, float low, float scale) {
+  using C = CutRoom<TEAM>;
+  constexpr int kOwn = C::kBins / TEAM;
+  const int rank = Team<TEAM>::rank(), lane = threadIdx.x & 63, wave = rank >> 6;
+  Cutoff cut{0, 0x7fffffff};
+  bool by_mass = a.top_k == 0;
+  float from = h.top, to = low, by = scale;  // the logits that are binned, and how
+  double mass_before = 0.;                   // of the logits above them
+  int count_before = 0;
+#pragma unroll 1
+  for (bool binned = true;; binned = false) {
+    if (!binned) {
+      team.sync();
+      m.clear(rank);
+      team.sync();
+      h.forget();
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone) {
+          const int b = C::bin_of(from - h.x[j], by);
+          unsafeAtomicAdd(&m.mass[b], h.weight(j));
+          if (a.top_k > 0) atomicAdd(&m.count[b], 1);
+        }
+      }
+      team.sync();
+    }
+    // sums before this thread's bins
+    double mass = 0.;
+    int count = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      mass += m.mass[rank * kOwn + i];
+      if (a.top_k > 0) count += m.count[rank * kOwn + i];
+    }
+    double run = sum_until<64>(mass);
+    int seen = a.top_k > 0 ? sum_until<64>(count) : 0;
+    if constexpr (TEAM > 64) {
+      if (lane == 63) {
+        m.wave_mass[wave] = run;
+        m.wave_count[wave] = seen;
+      }
+      team.sync();
+      double behind = 0.;
+      int passed = 0;
+      for (int i = 0; i < TEAM / 64; ++i) {
+        behind += i < wave ? m.wave_mass[i] : 0.;
+        passed += i < wave ? m.wave_count[i] : 0;
+        all += m.wave_count[i];
+      }
+      run += behind;
+      seen += passed;
+    } else {
+      all = of_lane(seen, 63);
+    }
+    run += mass_before - mass;
+    seen += count_before - count;
+    if (!by_mass && binned && all <= a.top_k) by_mass = true;  // top_k keeps all
+    if (by_mass && !(a.top_p < 1.)) break;
+    const double share = a.top_p * whole;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      const int b = rank * kOwn + i;
+      const double one = m.mass[b];
+      const int n = a.top_k > 0 ? m.count[b] : 0;
+      if (by_mass ? run < share && share <= run + one : seen < a.top_k && a.top_k <= seen + n) {
+        m.bin = b;
+        m.mass_before = run;
+        m.count_before = seen;
+        m.listed = 0;
+      }
+      run += one;
+      seen += n;
+    }
+    team.sync();
+    const int bin = m.bin;
+    h.forget();
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if (h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone && C::bin_of(from - h.x[j], by) == bin) {
+        const int at = atomicAdd(&m.listed, 1);
+        if (at < C::kList) {
+          m.key[at] = h.key(j);
+          m.index[at] = h.at(j);
+          m.weight[at] = h.weight(j);
+        }
+      }
+    }
+    team.sync();
+    const int listed = m.listed;
+    mass_before = m.mass_before;
+    count_before = m.count_before;
+    if (listed > C::kList) {
+      float most = kNone, least = -kNone;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const bool in = h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone && C::bin_of(from - h.x[j], by) == bin;
+        most = in && h.x[j] > most ? h.x[j] : most;
+        least = in && h.x[j] < least ? h.x[j] : least;
+      }
+      from = team.most(most);
+      to = team.all(least, [](float a, float b) { return a < b ? a : b; });
+      if (to < from) {
+        by = (float)C::kBins / (from - to);
+        continue;
+      }
+      const double one = m.weight[0];
+      const int ties = by_mass ? (int)__builtin_fmin(__builtin_ceil((share - mass_before) / one), (double)PCGRL_MAX_CLASSES) : a.top_k - count_before;
+      cut = cut_ties<T, TEAM, PER>(h, team, m.key[0], ties, &m.found);
+      whole = mass_before + (double)ties * one;
+    } else {
+      for (int i = rank; i < listed; i += TEAM) {
+        const uint32_t key = m.key[i];
+        const int index = m.index[i];
+        double before = mass_before;
+        int first = count_before;
+#pragma unroll 4
+        for (int o = 0; o < listed; ++o) {
+          const bool in = m.key[o] > key || (m.key[o] == key && m.index[o] < index);
+          before += in ? m.weight[o] : 0.;
+          first += in;
+        }
+        const double until = before + m.weight[i];
+        if (by_mass ? before < share && share <= until : first == a.top_k - 1) {
+          m.found = Cutoff{key, index};
+          m.mass_until = until;
+        }
+      }
+      team.sync();
+      cut = m.found;
+      whole = m.mass_until;
+    }
+    if (by_mass || !(a.top_p < 1.)) break;
+    by_mass = true;  // top_p, of what top_k has left
+    from = h.top;
+    to = low;
+    by = scale;
+    mass_before = 0.;
+    count_before = 0;
+  }
+  return cut;
+}
+
+template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(team_block<TEAM>()) void sample_kernel(SampleArgs a) {
+  using R = Row<T, TEAM, PER>;
+  constexpr int kTeams = team_block<TEAM>() / TEAM;
+  constexpr double kUnit = weight_unit<TEAM * PER>();
+  constexpr bool kBinned = HOW == kSampleCut && TEAM >= 64;
+  __shared__ double table[64], room[TEAM > 64 ? 2 * TEAM / 64 : 1];
+  __shared__ CutRoom<kBinned ? TEAM : 1> cut_room[kBinned ? kTeams : 1];
+  Team<TEAM> team{room};
+  if (HOW != kSampleBest) fill_powers(table, kUnit);
+  const bool searched = HOW == kSampleCut && (a.top_k > 0 || a.top_p < 1.);
+  for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
+    Held<T, TEAM, PER> h;
+    const int rank = team.rank_anew();
+    R::load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, rank, a.n, h.x);
+    float top = kNone, low = -kNone;
+    bool odd = false;  // a NaN or +infinity
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      top = __builtin_fmaxf(top, h.x[j]);
+      if (kBinned) low = __builtin_fminf(low, h.x[j] == kNone ? -kNone : h.x[j]);
+      odd |= !(h.x[j] < __builtin_huge_valf());
+    }
+    top = team.most(odd ? __builtin_huge_valf() : top);
+    if (!(top < __builtin_huge_valf()) || top == kNone) {
+      if (rank == 0) {
         a.actions[row] = -1;
-        if (a.log_probs) a.log_probs[row] = odd == 0 ? 0.f : __builtin_nanf("");
+        if (a.log_probs) a.log_probs[row] = top == kNone ? 0.f : __builtin_nanf("");
       }
       continue;
     }
@@ -207,150 +696,97 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
       int best = a.n;
 #pragma unroll
       for (int j = PER - 1; j >= 0; --j)
-        if (x[j] == top) best = R::at(j / R::VEC) + j % R::VEC;
+        if (h.x[j] == top) best = R::at(rank, j / R::VEC, j % R::VEC, a.n);
       best = team.least(best);
-      if (team.rank() == 0) {
+      if (rank == 0) {
         a.actions[row] = best;
         if (a.log_probs) a.log_probs[row] = 0.f;
       }
       continue;
     }
-    double w[PER], whole = 0.;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      w[j] = __builtin_rint(kUnit * pow2(((double)x[j] - (double)top) * a.slope));
-      whole += w[j];
+    h.rank = rank;
+    h.n = a.n;
+    h.top = top;
+    h.slope = a.slope;
+    h.table = table;
+    float scale = 0.f;
+    if constexpr (kBinned) {
+      if (searched) {
+        low = team.all(low, [](float a, float b) { return a < b ? a : b; });
+        const float range = __builtin_fminf(top - low, a.reach);
+        scale = range > 0.f ? (float)CutRoom<TEAM>::kBins / range : 0.f;
+        CutRoom<TEAM>& m = cut_room[threadIdx.x / TEAM % kTeams];
+        m.clear(rank);
+        team.sync();
+      }
     }
-    whole = team.sum(whole);
+    double piece[R::PIECES], mine = 0., before, here, w[PER];
+    h.forget();
+#pragma unroll
+    for (int c = 0; c < R::PIECES; ++c) {
+      piece[c] = 0.;
+#pragma unroll
+      for (int e = 0; e < R::VEC; ++e) {
+        const int j = c * R::VEC + e;
+        w[j] = h.weight(j);
+        piece[c] += w[j];
+        if constexpr (kBinned) {
+          if (searched) {
+            CutRoom<TEAM>& m = cut_room[threadIdx.x / TEAM % kTeams];
+            const int b = m.bin_of(top - h.x[j], scale);
+            if (w[j] > 0.) unsafeAtomicAdd(&m.mass[b], w[j]);
+            if (a.top_k > 0 && h.x[j] != kNone) atomicAdd(&m.count[b], 1);
+          }
+        }
+        part_end(j, piece[c]);
+      }
+      mine += piece[c];
+    }
+    const double whole = team.sum(mine, before, here);
     double kept = whole;
+    const double least = HOW == kSampleCut ? a.min_p * kUnit : 0.;
+    Cutoff cut{0, 0x7fffffff};
     if constexpr (HOW == kSampleCut) {
-      // The classes kept are those of a larger key than `edge` and the first `ties` of that key.
-      uint32_t edge = 0;
-      int ties = 0x7fffffff;
-      constexpr int kBits = 32 - T::kKeyShift;
-      auto key = [&](int j) { return key_of(x[j]) >> T::kKeyShift; };
-      auto count_from = [&](uint32_t k) {
-        int c = 0;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) c += key(j) >= k;
-        return team.sum(c);
-      };
-      auto sum_from = [&](uint32_t k) {
-        double s = 0.;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) s += key(j) >= k ? w[j] : 0.;
-        return team.sum(s);
-      };
-      auto weight_at = [&](uint32_t k) {
-        float v = kNone;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) v = key(j) == k ? x[j] : v;
-        v = team.most(v);
-        return __builtin_rint(kUnit * pow2(((double)v - (double)top) * a.slope));
-      };
-      if (a.top_k > 0 && count_from((key_of(kNone) >> T::kKeyShift) + 1) > a.top_k) {
-        for (int b = kBits - 1; b >= 0; --b) {
-          const uint32_t k = edge | (1u << b);
-          if (count_from(k) >= a.top_k) edge = k;
+      if constexpr (kBinned) {
+        if (searched) {
+          if (TEAM == 64) team.sync();
+          cut = cut_by_bins<T, TEAM, PER>(h, team, a, cut_room[threadIdx.x / TEAM % kTeams], whole, low, scale);
         }
-        ties = a.top_k - count_from(edge + 1);
-        kept = sum_from(edge + 1) + ties * weight_at(edge);
+      } else if constexpr (TEAM > 1) {
+        if (searched) cut = cut_by_halves<T, TEAM, PER>(h, team, a, whole, nullptr);
+      } else {
+        cut = cut_lane<T, PER>(h, a, w);
       }
-      if (a.top_p < 1.) {
-        const double share = a.top_p * kept;
-        uint32_t k2 = 0;
-        for (int b = kBits - 1; b >= 0; --b) {
-          const uint32_t k = k2 | (1u << b);
-          if (sum_from(k) >= share) k2 = k;
-        }
-        if (k2 >= edge) {
-          const double above = sum_from(k2 + 1), one = weight_at(k2);
-          int more = 1;                                      // classes of this key while the sum before them is below the share
-          if (one > 0.) more = (int)__builtin_fmin(__builtin_ceil((share - above) / one), 32768.);
-          ties = k2 == edge && ties < more ? ties : more;
-          edge = k2;
-        }
-      }
-      // the last class, by index, of those of the key `edge` that are kept
-      int last = 0x7fffffff;
-      auto count_at = [&](int until) {
-        int c = 0;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) c += key(j) == edge && R::at(j / R::VEC) + j % R::VEC <= until;
-        return team.sum(c);
-      };
-      if (ties < 32768 && count_at(a.n) > ties) {
-        int low = -1, high = a.n - 1;                        // count_at(low) < ties <= count_at(high)
-        while (high - low > 1) {
-          const int mid = (low + high) >> 1;
-          if (count_at(mid) < ties) low = mid; else high = mid;
-        }
-        last = high;
-      }
-      kept = 0.;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const bool in = key(j) > edge || (key(j) == edge && R::at(j / R::VEC) + j % R::VEC <= last);
-        const bool enough = pow2(((double)x[j] - (double)top) * a.slope) >= a.min_p;
-        w[j] = in && enough ? w[j] : 0.;
-        kept += w[j];
-      }
-      kept = team.sum(kept);
     }
-    // the first class whose running sum exceeds the target
+    // what is kept of a class's weight
+    auto kept_of = [&](const auto& in, int j, int index) {
+      const double v = in.weight(j);
+      const uint32_t key = in.key(j);
+      return HOW != kSampleCut || ((key > cut.key || (key == cut.key && index <= cut.index)) && v >= least) ? v : 0.;
+    };
+    if constexpr (HOW == kSampleCut) {
+      h.forget();
+      mine = 0.;
+#pragma unroll
+      for (int c = 0; c < R::PIECES; ++c) {
+        piece[c] = 0.;
+#pragma unroll
+        for (int e = 0; e < R::VEC; ++e) {
+          piece[c] += kept_of(h, c * R::VEC + e, R::at(rank, c, e, a.n));
+          part_end(c * R::VEC + e, piece[c]);
+        }
+        mine += piece[c];
+      }
+      kept = team.sum(mine, before, here);
+    }
     double u = (double)a.uniform[row];
     u = u >= 0. ? u : 0.;
     const double target = (u < 1. ? u : 1. - 0x1p-24) * kept;
-    int chosen = a.n;
-    double before = 0.;
-    bool here = true;
-    if constexpr (TEAM > 64) {
-      double mine = 0.;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) mine += w[j];
-      for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d);
-      if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = mine;
-      __syncthreads();
-      for (int i = 0; i < (int)(threadIdx.x >> 6); ++i) before += wave_sums[i];
-      here = before <= target && target < before + mine;
-    }
-    if (here) {
-#pragma unroll
-      for (int c = 0; c < R::PIECES; ++c) {
-        double mine = 0.;
-#pragma unroll
-        for (int e = 0; e < R::VEC; ++e) mine += w[c * R::VEC + e];
-        double until = mine;                                 // running sum over the lanes of a team
-        for (int d = 1; d < R::LANES; d <<= 1) {
-          const double o = __shfl_up(until, d, R::LANES);
-          until += (Team<TEAM>::rank() % R::LANES) >= d ? o : 0.;
-        }
-        double run = before + until - mine;
-        if (run <= target && target < before + until) {
-#pragma unroll
-          for (int e = 0; e < R::VEC; ++e) {
-            run += w[c * R::VEC + e];
-            if (run > target && chosen == a.n) chosen = R::at(c) + e;
-          }
-        }
-        before += __shfl(until, R::LANES - 1, R::LANES);
-      }
-    }
-    if constexpr (TEAM > 64) {
-      if (chosen < a.n) found = chosen;
-      __syncthreads();
-      chosen = found;
-    } else {
-      chosen = team.least(chosen);
-    }
-    chosen = (uint32_t)chosen < (uint32_t)a.n ? chosen : a.n - 1;
-    if (team.rank() == 0) {
-      a.actions[row] = chosen;
-      if (a.log_probs) {
-        const typename T::raw* at = static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride;
-        a.log_probs[row] = (float)(((double)T::load(at[chosen]) - (double)top) * a.inv_temperature - log(whole / kUnit));
-      }
-    }
+    h.forget();
+    find_class(h, piece, before, here, target, kept_of, [&](int at, float logit) {
+      a.actions[row] = at;
+      if (a.log_probs) a.log_probs[row] = (float)(((double)logit - (double)top) * a.inv_temperature - log(whole / kUnit));
+    });
   }
 }
 
@@ -382,8 +818,9 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
   using R = Row<T, TEAM, PER>;
   using raw = typename T::raw;
   __shared__ double room[TEAM > 64 ? 2 * TEAM / 64 : 1];
-  __shared__ double sums[kLossSums][team_block<TEAM>() / 64];
+  __shared__ double table[64], sums[kLossSums][team_block<TEAM>() / 64];
   Team<TEAM> team{room};
+  fill_powers(table, 1.);
   constexpr int kTeams = team_block<TEAM>() / TEAM;
   double part[kLossSums] = {};
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
@@ -392,26 +829,35 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     const int action = a.actions[row];
     const bool inside = action >= 0 && action < a.n;
     float x[PER];
-    R::load(logits, mask, a.n, x);
+    int rank = team.rank_anew();
+    R::load(logits, mask, rank, a.n, x);
     const float mine = inside && (!mask || mask[action] != 0) ? T::load(logits[action]) : kNone;
     float top = kNone;
+    bool odd = false;                     // a NaN or +infinity
 #pragma unroll
-    for (int j = 0; j < PER; ++j) top = x[j] > top ? x[j] : top;
-    top = team.most(top);
+    for (int j = 0; j < PER; ++j) {
+      top = __builtin_fmaxf(top, x[j]);
+      odd |= !(x[j] < __builtin_huge_valf());
+    }
+    top = team.most(odd ? __builtin_huge_valf() : top);
     const bool use = mine != kNone;       // (then something may be chosen)
     float w[PER];
     double whole = 0., spread = 0.;       // sums of the weights, and of the weights times their log2
+    forget_classes<TEAM, PER>(x, rank);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const double y = ((double)x[j] - (double)top) * a.slope, e = pow2(y);
-      w[j] = x[j] == kNone ? 0.f : (float)e;
-      whole += x[j] == kNone ? 0. : e;
-      spread += x[j] == kNone ? 0. : e * y;
+      const double y = ((double)x[j] - (double)top) * a.slope, e = power(table, y);
+      // (a class that may not be chosen has the weight of 2^-1000, nothing)
+      w[j] = (float)e;
+      done(w[j]);
+      whole += e;
+      spread = __builtin_fma(e, __builtin_fmax(y, -64000.), spread);
+      part_end(j, whole, spread);
     }
-    whole = team.sum(whole);
+    whole = top < __builtin_huge_valf() ? team.sum(whole) : __builtin_nan("");
     spread = team.sum(spread);
     const double log_whole = log(whole);
-    const double entropy = log_whole - 0.69314718055994530942 * (spread / whole);
+    const double entropy = log_whole - 0.69314718055994530942 / 64. * (spread / whole);
     const double logp = ((double)mine - (double)top) * a.inv_temperature - log_whole;
     double pull = 0.;                     // the policy loss's derivative by the log-probability
     if (use) {
@@ -420,7 +866,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
       const double ratio = exp(change);
       const bool clipped = a.old && ((adv > 0. && ratio > a.high) || (adv < 0. && ratio < a.low));
       pull = clipped ? 0. : -adv * ratio;
-      if (team.rank() == 0) {
+      if (rank == 0) {
         part[0] += 1.;
         part[1] += !a.old ? -adv * logp : clipped ? -adv * (adv > 0. ? a.high : a.low) : -adv * ratio;
         part[2] += entropy;
@@ -428,7 +874,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
         part[5] += clipped ? 1. : 0.;
       }
     }
-    if (team.rank() == 0) {
+    if (rank == 0) {
       if (a.values) {
         const double off = use ? (double)T::load(static_cast<const raw*>(a.values)[row]) - (double)a.returns[row] : 0.;
         part[3] += .5 * off * off;
@@ -441,15 +887,21 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
       const double by = a.scale * a.inv_temperature;
       const float k1 = (float)(by * pull), k2 = (float)(by * a.entropy_coef);
       const float inv = (float)(1. / whole), h = (float)(entropy - log_whole), slope = (float)a.inv_temperature;
-      float g[PER];
+      forget_classes<TEAM, PER>(x, rank);
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const float p = w[j] * inv;
-        const float around = (x[j] - top) * slope + h;      // log p + entropy
-        const bool chosen = R::at(j / R::VEC) + j % R::VEC == action;
-        g[j] = !use || x[j] == kNone ? 0.f : k2 * p * around + (chosen ? k1 - k1 * p : -(k1 * p));
+      for (int c = 0; c < R::PIECES; ++c) {
+        float g[R::VEC];
+#pragma unroll
+        for (int e = 0; e < R::VEC; ++e) {
+          const int j = c * R::VEC + e;
+          const float p = w[j] * inv;
+          const float around = (x[j] - top) * slope + h;    // log p + entropy
+          const bool chosen = R::at(rank, c, e, a.n) == action;
+          g[e] = !use || x[j] == kNone ? 0.f : k2 * p * around + (chosen ? k1 - k1 * p : -(k1 * p));
+        }
+        R::store(static_cast<raw*>(a.grad_logits) + row * a.grad_stride, rank, a.n, c, g);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      R::store(static_cast<raw*>(a.grad_logits) + row * a.grad_stride, a.n, g);
     }
   }
   if (!a.partial) return;
@@ -503,23 +955,23 @@ constexpr int kAdvantageAll = 0, kAdvantageSum = 1, kAdvantageApply = 2;
 constexpr int kAdvantageEach = 8;  // groups of a thread of the launch in the middle
 
 // (a factor of 0 is the end of an episode: what is behind it does not count, be it infinite or no number)
-__device__ inline double after_it(double factor, double term, double behind) { return factor == 0. ? term : __builtin_fma(factor, behind, term); }
+__device__ __forceinline__ double after_it(double factor, double term, double behind) { return factor == 0. ? term : __builtin_fma(factor, behind, term); }
 
 // Between the launches the factor and the term of group g + 1, and then the advantage behind group g, lie in the
 // first rows of group g's own advantages, which the last launch reads before it writes them.
-__device__ inline void put(float* at, int64_t n, double v) {
+__device__ __forceinline__ void put(float* at, int64_t n, double v) {
   const uint64_t u = (uint64_t)__double_as_longlong(v);
   at[0] = __uint_as_float((uint32_t)u);
   at[n] = __uint_as_float((uint32_t)(u >> 32));
 }
-__device__ inline double take(const float* at, int64_t n) {
+__device__ __forceinline__ double take(const float* at, int64_t n) {
   return __longlong_as_double((long long)((uint64_t)__float_as_uint(at[0]) | (uint64_t)__float_as_uint(at[n]) << 32));
 }
 
 // What the threads of a workgroup behind this one make of the advantage behind them all: thread c E + e has steps behind
 // those of thread (c - 1) E + e.  Sets `behind` to the advantage behind this thread's steps and returns that before the
 // workgroup's first; `factor_all`, if asked for, is multiplied by all factors.
-template <bool ALL> __device__ inline double join_steps(int envs_log2, double factor, double term, double& behind, double& factor_all, double (*factors)[64],
+template <bool ALL> __device__ __forceinline__ double join_steps(int envs_log2, double factor, double term, double& behind, double& factor_all, double (*factors)[64],
                                                         double (*terms)[64]) {
   constexpr int kWaves = kAdvantageThreads / 64;
   const int E = 1 << envs_log2, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
