@@ -63,11 +63,11 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 
 // Lets the compiler forget what it has computed from the classes of a thread: what it would keep from one pass over them to
 // the next takes more registers than there are.
-template <int TEAM, int PER> __device__ __forceinline__ void forget_classes(float (&x)[PER], int& rank) {
+template <int TEAM, int PER> __device__ __forceinline__ void forget_classes(float (&x)[PER], int& first) {
   if constexpr (TEAM >= 64) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) asm volatile("" : "+v"(x[j]));
-    asm volatile("" : "+v"(rank));
+    asm volatile("" : "+v"(first));
   }
 }
 
@@ -103,6 +103,18 @@ template <int LANES, typename V> __device__ __forceinline__ V sum_until(V v) {
   }
   return v;
 }
+
+// Whether logits have a NaN or +infinity among them: those are the largest of all bit patterns, with the sign or without it.
+// (A comparison for each logit takes three times as many instructions.)
+struct Oddity {
+  int most = (int)0x80000000;
+  uint32_t most_signed = 0;
+  __device__ __forceinline__ void look(float x) {
+    most = max(most, __float_as_int(x));
+    most_signed = max(most_signed, __float_as_uint(x));
+  }
+  __device__ __forceinline__ bool seen() const { return most >= 0x7f800000 || most_signed > 0xff800000u; }
+};
 
 // What the threads of a team know together.
 template <int TEAM> struct Team {
@@ -145,9 +157,10 @@ template <int TEAM> struct Team {
   __device__ int sum(int v) {
     return all(v, [](int a, int b) { return a + b; });
   }
-  // The sum, and what of it is in the wavefronts before this one and in this one.
-  __device__ double sum(double v, double& before, double& here) {
+  // The sum, and what of it is in the wavefronts before this one and in this one, to which each may have something to add.
+  __device__ __forceinline__ double sum(double v, double& before, double& here, const double* extra = nullptr) {
     here = over_lanes<kLanes>(v, [](double a, double b) { return a + b; });
+    if (extra) here += extra[TEAM > 64 ? rank() >> 6 : 0];
     before = 0.;
     if constexpr (TEAM > 64) {
       double *at = room + turn * kWaves, all = 0.;
@@ -172,7 +185,7 @@ template <int TEAM> struct Team {
 };
 
 // Powers of two by a table of 2^(i / 64), 64 doubles in LDS, times `unit`: power() is unit * 2^(z / 64) to 2^-44, with four terms
-// of the series of what is left of z, 18 instructions.
+// of the series of what is left of z, 17 instructions.
 __device__ __forceinline__ void fill_powers(double* table, double unit) {
   if (threadIdx.x < 64) table[threadIdx.x] = unit * 2. * pow2((double)threadIdx.x / 64. - 1.);
   __syncthreads();
@@ -185,60 +198,81 @@ __device__ __forceinline__ double power(const double* table, double z) {
   q = __builtin_fma(q, r, 2.1173137155464774e-07);        // 3
   q = __builtin_fma(q, r, 5.864904955056169e-05);         // 2
   q = __builtin_fma(q, r, 0.010830424696249145) * r;      // 1
-  const double of = table[n & 63], v = __builtin_fma(of, q, of);
-  return __hiloint2double(__double2hiint(v) + ((n & ~63) << 14), __double2loint(v));
+  const double of = table[n & 63];
+  return __builtin_ldexp(__builtin_fma(of, q, of), n >> 6);
 }
 
 // The classes of a thread: pieces of VEC neighbouring ones; each wavefront of a team has one stretch of the
-// row, in which its lanes' pieces lie side by side, so that running sums go from wavefront to wavefront.  A piece is read at
-// once, whatever its alignment; the one that the row ends in is read as the last VEC classes, of which
-// those of the piece before are left out.
+// row, in which its lanes' pieces lie side by side, so that running sums go from wavefront to wavefront.  The stretches are as
+// long as the row needs, to one piece, whatever the team could hold.  A piece is read at once, whatever its
+// alignment; the one that the row ends in is read as the last VEC classes, of which those of the piece before are left out.
 template <typename T, int TEAM, int PER> struct Row {
   static constexpr int VEC = PER < 16 / (int)sizeof(typename T::raw) ? PER : 16 / (int)sizeof(typename T::raw);
   static constexpr int PIECES = PER / VEC;
   static constexpr int LANES = TEAM < 64 ? TEAM : 64;
-  // first class of piece c of the team's thread r
-  static __device__ __forceinline__ int begin(int r, int c) {
-    return (r / LANES) * (LANES * PER) + (c * LANES + r % LANES) * VEC;
+  int first, pieces;  // the thread's first class, and the pieces of its wavefront
+  int n;
+  __device__ __forceinline__ Row(int rank, int n_classes) : n(n_classes) {
+    if constexpr (TEAM < 64) {
+      first = rank * VEC;
+      pieces = PIECES;
+    } else {
+      constexpr int W = TEAM / 64;
+      const int all = (n + 64 * VEC - 1) / (64 * VEC), w = __builtin_amdgcn_readfirstlane(rank >> 6), from = w * all / W;
+      pieces = (w + 1) * all / W - from;
+      first = (from * 64 + (rank & 63)) * VEC;
+    }
   }
+  __device__ __forceinline__ bool has(int c) const { return TEAM < 64 || c < pieces; }  // (the same for a wavefront)
+  __device__ __forceinline__ int begin(int c) const { return first + c * LANES * VEC; }
+  __device__ __forceinline__ bool owns(int c, int i) const { return i >= begin(c) && i < begin(c) + VEC; }
   // the class of element e of piece c
-  static __device__ __forceinline__ int at(int r, int c, int e, int n) {
-    const int first = begin(r, c);
-    return (TEAM > 1 && first > n - VEC ? n - VEC : first) + e;
+  __device__ __forceinline__ int at(int c, int e) const {
+    const int b = begin(c);
+    return (TEAM > 1 && b > n - VEC ? n - VEC : b) + e;
   }
   // Logits of the classes that may be chosen, kNone for the others.
-  static __device__ __forceinline__ void load(const typename T::raw* row, const uint8_t* mask, int r, int n, float (&x)[PER]) {
+  __device__ __forceinline__ void load(const typename T::raw* row, const uint8_t* mask, float (&x)[PER]) const {
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) {
-      const int first = begin(r, c), from = TEAM > 1 && first > n - VEC ? n - VEC : first;
-      typename T::raw v[VEC];
-      uint8_t m[VEC];
-      if (TEAM > 1 ? first < n : first + VEC <= n) {
-        __builtin_memcpy(v, row + from, sizeof(v));
-        if (mask) __builtin_memcpy(m, mask + from, sizeof(m));
-        else __builtin_memset(m, 1, sizeof(m));
+      const int b = begin(c), from = TEAM > 1 && b > n - VEC ? n - VEC : b;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[c * VEC + e] = m[e] == 0 || (TEAM > 1 && from + e < first) ? kNone : T::load(v[e]);
-      } else {
+      for (int e = 0; e < VEC; ++e) x[c * VEC + e] = kNone;
+      if (has(c) && (TEAM > 1 ? b < n : b + VEC <= n)) {
+        typename T::raw v[VEC];
+        __builtin_memcpy(v, row + from, sizeof(v));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[c * VEC + e] = T::load(v[e]);
+        if (mask) {
+          uint8_t m[VEC];
+          __builtin_memcpy(m, mask + from, sizeof(m));
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[c * VEC + e] = m[e] == 0 ? kNone : x[c * VEC + e];
+        }
+        if (TEAM > 1 && from < b) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[c * VEC + e] = from + e < b ? kNone : x[c * VEC + e];
+        }
+      } else if (TEAM == 1) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const int i = first + e;
-          x[c * VEC + e] = TEAM == 1 && i < n && (!mask || mask[i] != 0) ? T::load(row[i]) : kNone;
+          const int i = b + e;
+          if (i < n && (!mask || mask[i] != 0)) x[c * VEC + e] = T::load(row[i]);
         }
       }
     }
   }
-  static __device__ __forceinline__ void store(typename T::raw* row, int r, int n, int c, const float (&g)[VEC]) {
-    const int first = begin(r, c), from = TEAM > 1 && first > n - VEC ? n - VEC : first;
+  __device__ __forceinline__ void store(typename T::raw* row, int c, const float (&g)[VEC]) const {
+    const int b = begin(c), from = TEAM > 1 && b > n - VEC ? n - VEC : b;
     typename T::raw v[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[e] = T::store(g[e]);
-    if (first + VEC <= n) {
-      __builtin_memcpy(row + first, v, sizeof(v));
-    } else if (first < n) {
+    if (b + VEC <= n) {
+      __builtin_memcpy(row + b, v, sizeof(v));
+    } else if (b < n) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (from + e >= first && from + e < n) row[from + e] = v[e];
+        if (from + e >= b && from + e < n) row[from + e] = v[e];
     }
   }
 };
@@ -253,6 +287,9 @@ template <typename... V> __device__ __forceinline__ void part_end(int j, V&... s
   }
 }
 
+// Wavefronts that a SIMD has room for at least: two workgroups of 512 threads a compute unit, one of which waits for its rows
+// while the other computes.
+template <int TEAM> constexpr int team_waves() { return TEAM >= 64 ? 4 : 1; }
 template <int TEAM> constexpr int team_block() { return TEAM > 64 ? TEAM : 256; }
 
 // ---- actions drawn from logits
@@ -297,6 +334,8 @@ template <int TEAM> struct CutRoom {
   int count[kBins];
   uint32_t key[kList];
   int index[kList];
+  uint8_t wave[kList];
+  double extra[TEAM / 64];
   double wave_mass[TEAM / 64];
   int wave_count[TEAM / 64];
   double mass_before, mass_until;
@@ -319,19 +358,19 @@ template <> struct CutRoom<1> {};
 template <typename T, int TEAM, int PER> struct Held {
   using R = Row<T, TEAM, PER>;
   float x[PER];
-  int rank, n;
+  R row;
   float top;
+  __device__ __forceinline__ Held(int rank, int n) : row(rank, n) {}
+  __device__ __forceinline__ explicit Held(const R& r) : row(r) {}
   double slope;
   const double* table;
   // (the two zeros are equal)
   __device__ __forceinline__ uint32_t key(int j) const { return key_of(x[j] + 0.f) >> T::kKeyShift; }
   __device__ __forceinline__ double weight(int j) const { return __builtin_rint(power(table, ((double)x[j] - (double)top) * slope)); }
-  __device__ __forceinline__ int at(int j) const { return R::at(rank, j / R::VEC, j % R::VEC, n); }
+  __device__ __forceinline__ int at(int j) const { return row.at(j / R::VEC, j % R::VEC); }
   // One of the pieces.
   template <int VEC> __device__ __forceinline__ Held<T, TEAM, VEC> piece(int which) const {
-    Held<T, TEAM, VEC> p;
-    p.rank = rank;
-    p.n = n;
+    Held<T, TEAM, VEC> p(0, VEC);  // (its row is not asked for)
     p.top = top;
     p.slope = slope;
     p.table = table;
@@ -349,7 +388,7 @@ template <typename T, int TEAM, int PER> struct Held {
     }
     return p;
   }
-  __device__ __forceinline__ void forget() { forget_classes<TEAM, PER>(x, rank); }
+  __device__ __forceinline__ void forget() { forget_classes<TEAM, PER>(x, row.first); }
 };
 template <typename T> __device__ __forceinline__ uint32_t no_key() { return key_of(kNone) >> T::kKeyShift; }
 
@@ -381,7 +420,7 @@ __device__ __forceinline__ void find_class(const Held<T, TEAM, PER>& h, const do
     float logit = 0.f;
 #pragma unroll
     for (int e = 0; e < R::VEC; ++e) {
-      const int index = R::at(h.rank, which, e, h.n);
+      const int index = h.row.at(which, e);
       run += value(in, e, index);
       float x = in.x[e];
       asm("" : "+v"(x));  // (else it becomes an address chosen among the classes, and they go to memory)
@@ -514,6 +553,46 @@ __device__ __forceinline__ Cutoff cut_by_halves(Held<T, TEAM, PER>& h, Team<TEAM
   return cut_ties<T, TEAM, PER>(h, team, edge, ties, shared);
 }
 
+// The sums before a thread's bins.
+template <int TEAM> struct BinSums {
+  double run;
+  int seen, all;
+  __device__ __forceinline__ BinSums(Team<TEAM>& team, CutRoom<TEAM>& m, int rank, bool counted) {
+    constexpr int kOwn = CutRoom<TEAM>::kBins / TEAM;
+    const int lane = threadIdx.x & 63, wave = rank >> 6;
+    double mass = 0.;
+    int count = 0;
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      mass += m.mass[rank * kOwn + i];
+      if (counted) count += m.count[rank * kOwn + i];
+    }
+    run = sum_until<64>(mass);
+    seen = counted ? sum_until<64>(count) : 0;
+    if constexpr (TEAM > 64) {
+      if (lane == 63) {
+        m.wave_mass[wave] = run;
+        m.wave_count[wave] = seen;
+      }
+      team.sync();
+      double behind = 0.;
+      int passed = 0;
+      for (int i = 0; i < TEAM / 64; ++i) {
+        behind += i < wave ? m.wave_mass[i] : 0.;
+        passed += i < wave ? m.wave_count[i] : 0;
+        all += m.wave_count[i];
+      }
+      run += behind;
+      seen += passed;
+    } else {
+      all = of_lane(seen, 63);
+    }
+    run -= mass;
+    seen -= count;
+  }
+};
+
 // By bins: the weights (for top_k the numbers) of a row's classes are added up in LDS in bins of equal width from the
 // largest logit down to the smallest one, or to where weights vanish; the bin in which the sum from the
 // top reaches what is looked for is listed, and each of its few classes is ranked against the others.  Three passes over the
@@ -523,7 +602,7 @@ template <typename T, int TEAM, int PER>
 __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double whole, float low, float scale) {
   using C = CutRoom<TEAM>;
   constexpr int kOwn = C::kBins / TEAM;
-  const int rank = Team<TEAM>::rank(), lane = threadIdx.x & 63, wave = rank >> 6;
+  const int rank = Team<TEAM>::rank();
   Cutoff cut{0, 0x7fffffff};
   bool by_mass = a.top_k == 0;
   float from = h.top, to = low, by = scale;  // the logits that are binned, and how
@@ -546,36 +625,10 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
       }
       team.sync();
     }
-    // sums before this thread's bins
-    double mass = 0.;
-    int count = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      mass += m.mass[rank * kOwn + i];
-      if (a.top_k > 0) count += m.count[rank * kOwn + i];
-    }
-    double run = sum_until<64>(mass);
-    int seen = a.top_k > 0 ? sum_until<64>(count) : 0;
-    if constexpr (TEAM > 64) {
-      if (lane == 63) {
-        m.wave_mass[wave] = run;
-        m.wave_count[wave] = seen;
-      }
-      team.sync();
-      double behind = 0.;
-      int passed = 0;
-      for (int i = 0; i < TEAM / 64; ++i) {
-        behind += i < wave ? m.wave_mass[i] : 0.;
-        passed += i < wave ? m.wave_count[i] : 0;
-        all += m.wave_count[i];
-      }
-      run += behind;
-      seen += passed;
-    } else {
-      all = of_lane(seen, 63);
-    }
-    run += mass_before - mass;
-    seen += count_before - count;
+    const BinSums<TEAM> sums(team, m, rank, a.top_k > 0);
+    const int all = sums.all;
+    double run = sums.run + mass_before;
+    int seen = sums.seen + count_before;
     if (!by_mass && binned && all <= a.top_k) by_mass = true;  // top_k keeps all
     if (by_mass && !(a.top_p < 1.)) break;
     const double share = a.top_p * whole;
@@ -598,6 +651,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
     h.forget();
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
+      if (!h.row.has(j / Held<T, TEAM, PER>::R::VEC)) continue;
       if (h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone && C::bin_of(from - h.x[j], by) == bin) {
         const int at = atomicAdd(&m.listed, 1);
         if (at < C::kList) {
@@ -662,7 +716,72 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
   return cut;
 }
 
-template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(team_block<TEAM>()) void sample_kernel(SampleArgs a) {
+// The same for top_p alone, which has the classes of the bins above added up in the pass that lists the bin: sets `mine` to what
+// of this thread's classes is kept outside that bin, m.extra to what each wavefront has in it.  False if the list does not
+// hold the bin.
+template <typename T, int TEAM, int PER>
+__device__ __forceinline__ bool share_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>& team, CutRoom<TEAM>& m, double share, double least, float scale, double& mine) {
+  using C = CutRoom<TEAM>;
+  using R = Row<T, TEAM, PER>;
+  constexpr int kOwn = C::kBins / TEAM;
+  const int rank = Team<TEAM>::rank();
+  const BinSums<TEAM> sums(team, m, rank, false);
+  double run = sums.run;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const double one = m.mass[rank * kOwn + i];
+    if (run < share && share <= run + one) {
+      m.bin = rank * kOwn + i;
+      m.mass_before = run;
+      m.listed = 0;
+    }
+    run += one;
+  }
+  if (rank < TEAM / 64) m.extra[rank] = 0.;
+  team.sync();
+  const int bin = m.bin;
+  h.forget();
+  mine = 0.;
+#pragma unroll
+  for (int c = 0; c < R::PIECES; ++c) {
+    if (!h.row.has(c)) continue;
+#pragma unroll
+    for (int e = 0; e < R::VEC; ++e) {
+      const int j = c * R::VEC + e, b = C::bin_of(h.top - h.x[j], scale);
+      const double w = h.weight(j);
+      mine += b < bin && w >= least ? w : 0.;
+      if (b == bin && h.x[j] != kNone) {
+        const int at = atomicAdd(&m.listed, 1);
+        if (at < C::kList) {
+          m.key[at] = h.key(j);
+          m.index[at] = h.at(j);
+          m.weight[at] = w;
+          m.wave[at] = (uint8_t)(rank >> 6);
+        }
+      }
+      part_end(j, mine);
+    }
+  }
+  team.sync();
+  const int listed = m.listed;
+  if (listed > C::kList) return false;
+  for (int i = rank; i < listed; i += TEAM) {
+    const uint32_t key = m.key[i];
+    const int index = m.index[i];
+    double before = m.mass_before;
+#pragma unroll 4
+    for (int o = 0; o < listed; ++o) before += m.key[o] > key || (m.key[o] == key && m.index[o] < index) ? m.weight[o] : 0.;
+    const double w = m.weight[i];
+    if (before < share) {
+      if (share <= before + w) m.found = Cutoff{key, index};
+      if (w >= least) unsafeAtomicAdd(&m.extra[m.wave[i]], w);
+    }
+  }
+  team.sync();
+  return true;
+}
+
+template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), team_waves<TEAM>()) void sample_kernel(SampleArgs a) {
   using R = Row<T, TEAM, PER>;
   constexpr int kTeams = team_block<TEAM>() / TEAM;
   constexpr double kUnit = weight_unit<TEAM * PER>();
@@ -673,18 +792,18 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
   if (HOW != kSampleBest) fill_powers(table, kUnit);
   const bool searched = HOW == kSampleCut && (a.top_k > 0 || a.top_p < 1.);
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
-    Held<T, TEAM, PER> h;
     const int rank = team.rank_anew();
-    R::load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, rank, a.n, h.x);
+    Held<T, TEAM, PER> h(rank, a.n);
+    h.row.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, h.x);
     float top = kNone, low = -kNone;
-    bool odd = false;  // a NaN or +infinity
+    Oddity odd;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       top = __builtin_fmaxf(top, h.x[j]);
       if (kBinned) low = __builtin_fminf(low, h.x[j] == kNone ? -kNone : h.x[j]);
-      odd |= !(h.x[j] < __builtin_huge_valf());
+      odd.look(h.x[j]);
     }
-    top = team.most(odd ? __builtin_huge_valf() : top);
+    top = team.most(odd.seen() ? __builtin_huge_valf() : top);
     if (!(top < __builtin_huge_valf()) || top == kNone) {
       if (rank == 0) {
         a.actions[row] = -1;
@@ -696,7 +815,7 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
       int best = a.n;
 #pragma unroll
       for (int j = PER - 1; j >= 0; --j)
-        if (h.x[j] == top) best = R::at(rank, j / R::VEC, j % R::VEC, a.n);
+        if (h.x[j] == top) best = h.at(j);
       best = team.least(best);
       if (rank == 0) {
         a.actions[row] = best;
@@ -704,8 +823,6 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
       }
       continue;
     }
-    h.rank = rank;
-    h.n = a.n;
     h.top = top;
     h.slope = a.slope;
     h.table = table;
@@ -725,6 +842,7 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
 #pragma unroll
     for (int c = 0; c < R::PIECES; ++c) {
       piece[c] = 0.;
+      if (!h.row.has(c)) continue;
 #pragma unroll
       for (int e = 0; e < R::VEC; ++e) {
         const int j = c * R::VEC + e;
@@ -746,42 +864,54 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
     double kept = whole;
     const double least = HOW == kSampleCut ? a.min_p * kUnit : 0.;
     Cutoff cut{0, 0x7fffffff};
-    if constexpr (HOW == kSampleCut) {
-      if constexpr (kBinned) {
-        if (searched) {
-          if (TEAM == 64) team.sync();
-          cut = cut_by_bins<T, TEAM, PER>(h, team, a, cut_room[threadIdx.x / TEAM % kTeams], whole, low, scale);
-        }
-      } else if constexpr (TEAM > 1) {
-        if (searched) cut = cut_by_halves<T, TEAM, PER>(h, team, a, whole, nullptr);
-      } else {
-        cut = cut_lane<T, PER>(h, a, w);
-      }
-    }
     // what is kept of a class's weight
     auto kept_of = [&](const auto& in, int j, int index) {
       const double v = in.weight(j);
       const uint32_t key = in.key(j);
       return HOW != kSampleCut || ((key > cut.key || (key == cut.key && index <= cut.index)) && v >= least) ? v : 0.;
     };
-    if constexpr (HOW == kSampleCut) {
-      h.forget();
-      mine = 0.;
-#pragma unroll
-      for (int c = 0; c < R::PIECES; ++c) {
-        piece[c] = 0.;
-#pragma unroll
-        for (int e = 0; e < R::VEC; ++e) {
-          piece[c] += kept_of(h, c * R::VEC + e, R::at(rank, c, e, a.n));
-          part_end(c * R::VEC + e, piece[c]);
-        }
-        mine += piece[c];
-      }
-      kept = team.sum(mine, before, here);
-    }
     double u = (double)a.uniform[row];
     u = u >= 0. ? u : 0.;
-    const double target = (u < 1. ? u : 1. - 0x1p-24) * kept;
+    u = u < 1. ? u : 1. - 0x1p-24;
+    if constexpr (HOW == kSampleCut) {
+      bool summed = false;  // what is kept, for each wavefront
+      if constexpr (kBinned) {
+        if (searched) {
+          CutRoom<TEAM>& m = cut_room[threadIdx.x / TEAM % kTeams];
+          if (TEAM == 64) team.sync();
+          if (a.top_k == 0) {
+            summed = share_by_bins<T, TEAM, PER>(h, team, m, a.top_p * whole, least, scale, mine);
+            if (summed) {
+              cut = m.found;
+              kept = team.sum(mine, before, here, m.extra);
+            }
+          }
+          if (!summed) cut = cut_by_bins<T, TEAM, PER>(h, team, a, m, whole, low, scale);
+        }
+      } else if constexpr (TEAM > 1) {
+        if (searched) cut = cut_by_halves<T, TEAM, PER>(h, team, a, whole, nullptr);
+      } else {
+        cut = cut_lane<T, PER>(h, a, w);
+      }
+      // for each piece: in all wavefronts, or in the one where the running sum exceeds the target
+      if (!summed || (before <= u * kept && u * kept < before + here)) {
+        h.forget();
+        mine = 0.;
+#pragma unroll
+        for (int c = 0; c < R::PIECES; ++c) {
+          piece[c] = 0.;
+          if (!h.row.has(c)) continue;
+#pragma unroll
+          for (int e = 0; e < R::VEC; ++e) {
+            piece[c] += kept_of(h, c * R::VEC + e, h.row.at(c, e));
+            part_end(c * R::VEC + e, piece[c]);
+          }
+          mine += piece[c];
+        }
+      }
+      if (!summed) kept = team.sum(mine, before, here);
+    }
+    const double target = u * kept;
     h.forget();
     find_class(h, piece, before, here, target, kept_of, [&](int at, float logit) {
       a.actions[row] = at;
@@ -814,7 +944,7 @@ struct LossArgs {
 constexpr int kLossSums = 6;  // rows, policy loss, entropy, value loss, divergence, clipped rows
 constexpr int kLossBlocks = 2048;
 
-template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>()) void loss_kernel(LossArgs a) {
+template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>(), team_waves<TEAM>()) void loss_kernel(LossArgs a) {
   using R = Row<T, TEAM, PER>;
   using raw = typename T::raw;
   __shared__ double room[TEAM > 64 ? 2 * TEAM / 64 : 1];
@@ -829,30 +959,36 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     const int action = a.actions[row];
     const bool inside = action >= 0 && action < a.n;
     float x[PER];
-    int rank = team.rank_anew();
-    R::load(logits, mask, rank, a.n, x);
+    const int rank = team.rank_anew();
+    R of(rank, a.n);
+    of.load(logits, mask, x);
     const float mine = inside && (!mask || mask[action] != 0) ? T::load(logits[action]) : kNone;
     float top = kNone;
-    bool odd = false;                     // a NaN or +infinity
+    Oddity odd;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       top = __builtin_fmaxf(top, x[j]);
-      odd |= !(x[j] < __builtin_huge_valf());
+      odd.look(x[j]);
     }
-    top = team.most(odd ? __builtin_huge_valf() : top);
+    top = team.most(odd.seen() ? __builtin_huge_valf() : top);
     const bool use = mine != kNone;       // (then something may be chosen)
     float w[PER];
     double whole = 0., spread = 0.;       // sums of the weights, and of the weights times their log2
-    forget_classes<TEAM, PER>(x, rank);
+    forget_classes<TEAM, PER>(x, of.first);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const double y = ((double)x[j] - (double)top) * a.slope, e = power(table, y);
-      // (a class that may not be chosen has the weight of 2^-1000, nothing)
-      w[j] = (float)e;
-      done(w[j]);
-      whole += e;
-      spread = __builtin_fma(e, __builtin_fmax(y, -64000.), spread);
-      part_end(j, whole, spread);
+    for (int c = 0; c < R::PIECES; ++c) {
+      if (!of.has(c)) continue;
+#pragma unroll
+      for (int i = 0; i < R::VEC; ++i) {
+        const int j = c * R::VEC + i;
+        const double y = ((double)x[j] - (double)top) * a.slope, e = power(table, y);
+        // (a class that may not be chosen has the weight of 2^-1000, nothing)
+        w[j] = (float)e;
+        done(w[j]);
+        whole += e;
+        spread = __builtin_fma(e, __builtin_fmax(y, -64000.), spread);
+        part_end(j, whole, spread);
+      }
     }
     whole = top < __builtin_huge_valf() ? team.sum(whole) : __builtin_nan("");
     spread = team.sum(spread);
@@ -863,7 +999,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     if (use) {
       const double adv = (double)a.advantages[row];
       const double change = a.old ? logp - (double)a.old[row] : 0.;
-      const double ratio = exp(change);
+      const double ratio = change == change ? power(table, __builtin_fmin(change * (64. * 1.44269504088896340736), 128000.)) : change;
       const bool clipped = a.old && ((adv > 0. && ratio > a.high) || (adv < 0. && ratio < a.low));
       pull = clipped ? 0. : -adv * ratio;
       if (rank == 0) {
@@ -884,22 +1020,28 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
       if (a.entropies) a.entropies[row] = use ? (float)entropy : 0.f;
     }
     if (a.grad_logits) {
-      const double by = a.scale * a.inv_temperature;
-      const float k1 = (float)(by * pull), k2 = (float)(by * a.entropy_coef);
-      const float inv = (float)(1. / whole), h = (float)(entropy - log_whole), slope = (float)a.inv_temperature;
-      forget_classes<TEAM, PER>(x, rank);
+      // scale / temperature * p (entropy_coef (log p + entropy) - pull) for each class; the lane of the one chosen, which has
+      // pull added, writes it once more
+      const double by = a.scale * a.inv_temperature, part_of = 1. / whole, bonus = by * a.entropy_coef, h = entropy - log_whole;
+      const double p = power(table, ((double)mine - (double)top) * a.slope) * part_of;
+      const float inv = (float)part_of, least = __builtin_fmaxf((float)(-1000. / a.inv_temperature), -3.4028235e38f);
+      const float k3 = (float)(bonus * a.inv_temperature), k4 = (float)(bonus * h - by * pull);
+      const float chosen = (float)(bonus * p * (logp + entropy) + by * pull * (1. - p));
+      raw* grad = static_cast<raw*>(a.grad_logits) + row * a.grad_stride;
+      forget_classes<TEAM, PER>(x, of.first);
 #pragma unroll
       for (int c = 0; c < R::PIECES; ++c) {
+        if (!of.has(c)) continue;
         float g[R::VEC];
 #pragma unroll
         for (int e = 0; e < R::VEC; ++e) {
           const int j = c * R::VEC + e;
-          const float p = w[j] * inv;
-          const float around = (x[j] - top) * slope + h;    // log p + entropy
-          const bool chosen = R::at(rank, c, e, a.n) == action;
-          g[e] = !use || x[j] == kNone ? 0.f : k2 * p * around + (chosen ? k1 - k1 * p : -(k1 * p));
+          // (of a class that may not be chosen w is 0, and the rest has to be a number)
+          g[e] = w[j] * inv * __builtin_fmaf(k3, __builtin_fmaxf(x[j] - top, least), k4);
+          if (!use) g[e] = 0.f;
         }
-        R::store(static_cast<raw*>(a.grad_logits) + row * a.grad_stride, rank, a.n, c, g);
+        of.store(grad, c, g);
+        if (use && of.owns(c, action)) grad[action] = T::store(chosen);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
