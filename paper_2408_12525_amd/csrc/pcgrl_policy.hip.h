@@ -93,13 +93,26 @@ template <int LANES, typename V, typename Op> __device__ __forceinline__ V over_
   }
   return v;
 }
-// Sum over the lanes before and including this one, of every LANES.
+// Sum over the lanes before and including this one, of every LANES: within rows of 16 lanes by shifts that bring in zeros, then
+// with what the rows before have.
 template <int LANES, typename V> __device__ __forceinline__ V sum_until(V v) {
-  const int lane = threadIdx.x & (LANES - 1);
-#pragma unroll
-  for (int d = 1; d < LANES; d <<= 1) {
-    const V o = __shfl_up(v, d, LANES);
-    v += lane >= d ? o : (V)0;
+  if constexpr (LANES == 8) {
+    const int lane = threadIdx.x & 7;
+    V o = moved<0x111>(v);
+    v += lane >= 1 ? o : (V)0;
+    o = moved<0x112>(v);
+    v += lane >= 2 ? o : (V)0;
+    o = moved<0x114>(v);
+    v += lane >= 4 ? o : (V)0;
+  }
+  if constexpr (LANES == 64) {
+    v += moved<0x111>(v);
+    v += moved<0x112>(v);
+    v += moved<0x114>(v);
+    v += moved<0x118>(v);
+    const V a = of_lane(v, 15), b = a + of_lane(v, 31), c = b + of_lane(v, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    v += row == 0 ? (V)0 : row == 1 ? a : row == 2 ? b : c;
   }
   return v;
 }
@@ -179,6 +192,24 @@ template <int TEAM> struct Team {
   __device__ int least(int v) {
     return all(v, [](int a, int b) { return a < b ? a : b; });
   }
+  // The largest of one and the smallest of the other, at once; orders LDS.
+  __device__ __forceinline__ void most_and_least(float& most, float& least) {
+    most = over_lanes<kLanes>(most, [](float a, float b) { return a > b ? a : b; });
+    least = over_lanes<kLanes>(least, [](float a, float b) { return a < b ? a : b; });
+    if constexpr (TEAM > 64) {
+      float2* at = reinterpret_cast<float2*>(room + turn * kWaves);
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = float2{most, least};
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        most = __builtin_fmaxf(most, at[i].x);
+        least = __builtin_fminf(least, at[i].y);
+      }
+    } else {
+      sync();
+    }
+  }
   __device__ float most(float v) {
     return all(v, [](float a, float b) { return a > b ? a : b; });
   }
@@ -186,9 +217,9 @@ template <int TEAM> struct Team {
 
 // Powers of two by a table of 2^(i / 64), 64 doubles in LDS, times `unit`: power() is unit * 2^(z / 64) to 2^-44, with four terms
 // of the series of what is left of z, 17 instructions.
-__device__ __forceinline__ void fill_powers(double* table, double unit) {
+template <int TEAM> __device__ __forceinline__ void fill_powers(double* table, double unit) {
   if (threadIdx.x < 64) table[threadIdx.x] = unit * 2. * pow2((double)threadIdx.x / 64. - 1.);
-  __syncthreads();
+  if (TEAM <= 64) __syncthreads();  // (larger teams have a barrier for their largest logit before they read it)
 }
 __device__ __forceinline__ double power(const double* table, double z) {
   z = __builtin_fmax(z, -64000.);
@@ -222,6 +253,12 @@ template <typename T, int TEAM, int PER> struct Row {
       pieces = (w + 1) * all / W - from;
       first = (from * 64 + (rank & 63)) * VEC;
     }
+  }
+  // the wavefront of a class: the last one that begins at its piece or before
+  __device__ __forceinline__ int wave_of(int index) const {
+    constexpr int W = TEAM < 64 ? 1 : TEAM / 64;
+    const int all = (n + 64 * VEC - 1) / (64 * VEC), piece = index / (64 * VEC);
+    return ((piece + 1) * W - 1) / all;
   }
   __device__ __forceinline__ bool has(int c) const { return TEAM < 64 || c < pieces; }  // (the same for a wavefront)
   __device__ __forceinline__ int begin(int c) const { return first + c * LANES * VEC; }
@@ -329,18 +366,33 @@ struct Cutoff {
 // LDS of a team that looks for it: weights and numbers of classes in bins of falling logits, and the classes of one bin.
 template <int TEAM> struct CutRoom {
   static constexpr int kBins = TEAM == 64 ? 512 : 2048, kList = TEAM == 64 ? 128 : 512;
+  struct alignas(16) Entry {
+    uint64_t order;  // the key, and below it the index turned round: what is kept first is larger
+    double weight;
+  };
+  Entry list[kList];
   double mass[kBins];
-  double weight[kList];
   int count[kBins];
-  uint32_t key[kList];
-  int index[kList];
-  uint8_t wave[kList];
   double extra[TEAM / 64];
   double wave_mass[TEAM / 64];
   int wave_count[TEAM / 64];
   double mass_before, mass_until;
   int bin, count_before, listed;
   Cutoff found;
+  __device__ __forceinline__ void put(uint32_t key, int index, double weight) {
+    const int at = atomicAdd(&listed, 1);
+    if (at < kList) list[at] = Entry{(uint64_t)key << 32 | (uint32_t)~index, weight};
+  }
+  static __device__ __forceinline__ Cutoff cutoff(uint64_t order) { return Cutoff{(uint32_t)(order >> 32), (int)~(uint32_t)order}; }
+  // Weights and number of the listed classes before the one given.
+  __device__ __forceinline__ void rank_of(uint64_t order, double& before, int& first) const {
+#pragma unroll 8
+    for (int i = 0; i < listed; ++i) {
+      const Entry e = list[i];
+      before += e.order > order ? e.weight : 0.;
+      first += e.order > order;
+    }
+  }
   __device__ __forceinline__ void clear(int rank) {
     for (int b = rank; b < kBins; b += TEAM) {
       mass[b] = 0.;
@@ -653,12 +705,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
     for (int j = 0; j < PER; ++j) {
       if (!h.row.has(j / Held<T, TEAM, PER>::R::VEC)) continue;
       if (h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone && C::bin_of(from - h.x[j], by) == bin) {
-        const int at = atomicAdd(&m.listed, 1);
-        if (at < C::kList) {
-          m.key[at] = h.key(j);
-          m.index[at] = h.at(j);
-          m.weight[at] = h.weight(j);
-        }
+        m.put(h.key(j), h.at(j), h.weight(j));
       }
     }
     team.sync();
@@ -679,25 +726,19 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
         by = (float)C::kBins / (from - to);
         continue;
       }
-      const double one = m.weight[0];
+      const double one = m.list[0].weight;
       const int ties = by_mass ? (int)__builtin_fmin(__builtin_ceil((share - mass_before) / one), (double)PCGRL_MAX_CLASSES) : a.top_k - count_before;
-      cut = cut_ties<T, TEAM, PER>(h, team, m.key[0], ties, &m.found);
+      cut = cut_ties<T, TEAM, PER>(h, team, C::cutoff(m.list[0].order).key, ties, &m.found);
       whole = mass_before + (double)ties * one;
     } else {
       for (int i = rank; i < listed; i += TEAM) {
-        const uint32_t key = m.key[i];
-        const int index = m.index[i];
+        const typename C::Entry e = m.list[i];
         double before = mass_before;
         int first = count_before;
-#pragma unroll 4
-        for (int o = 0; o < listed; ++o) {
-          const bool in = m.key[o] > key || (m.key[o] == key && m.index[o] < index);
-          before += in ? m.weight[o] : 0.;
-          first += in;
-        }
-        const double until = before + m.weight[i];
+        m.rank_of(e.order, before, first);
+        const double until = before + e.weight;
         if (by_mass ? before < share && share <= until : first == a.top_k - 1) {
-          m.found = Cutoff{key, index};
+          m.found = C::cutoff(e.order);
           m.mass_until = until;
         }
       }
@@ -751,13 +792,7 @@ __device__ __forceinline__ bool share_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
       const double w = h.weight(j);
       mine += b < bin && w >= least ? w : 0.;
       if (b == bin && h.x[j] != kNone) {
-        const int at = atomicAdd(&m.listed, 1);
-        if (at < C::kList) {
-          m.key[at] = h.key(j);
-          m.index[at] = h.at(j);
-          m.weight[at] = w;
-          m.wave[at] = (uint8_t)(rank >> 6);
-        }
+        m.put(h.key(j), h.at(j), w);
       }
       part_end(j, mine);
     }
@@ -766,15 +801,14 @@ __device__ __forceinline__ bool share_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
   const int listed = m.listed;
   if (listed > C::kList) return false;
   for (int i = rank; i < listed; i += TEAM) {
-    const uint32_t key = m.key[i];
-    const int index = m.index[i];
+    const typename C::Entry e = m.list[i];
     double before = m.mass_before;
-#pragma unroll 4
-    for (int o = 0; o < listed; ++o) before += m.key[o] > key || (m.key[o] == key && m.index[o] < index) ? m.weight[o] : 0.;
-    const double w = m.weight[i];
+    int first = 0;
+    m.rank_of(e.order, before, first);
     if (before < share) {
-      if (share <= before + w) m.found = Cutoff{key, index};
-      if (w >= least) unsafeAtomicAdd(&m.extra[m.wave[i]], w);
+      const Cutoff it = C::cutoff(e.order);
+      if (share <= before + e.weight) m.found = it;
+      if (e.weight >= least) unsafeAtomicAdd(&m.extra[h.row.wave_of(it.index)], e.weight);
     }
   }
   team.sync();
@@ -789,7 +823,7 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
   __shared__ double table[64], room[TEAM > 64 ? 2 * TEAM / 64 : 1];
   __shared__ CutRoom<kBinned ? TEAM : 1> cut_room[kBinned ? kTeams : 1];
   Team<TEAM> team{room};
-  if (HOW != kSampleBest) fill_powers(table, kUnit);
+  if (HOW != kSampleBest) fill_powers<TEAM>(table, kUnit);
   const bool searched = HOW == kSampleCut && (a.top_k > 0 || a.top_p < 1.);
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
     const int rank = team.rank_anew();
@@ -803,7 +837,13 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
       if (kBinned) low = __builtin_fminf(low, h.x[j] == kNone ? -kNone : h.x[j]);
       odd.look(h.x[j]);
     }
-    top = team.most(odd.seen() ? __builtin_huge_valf() : top);
+    top = odd.seen() ? __builtin_huge_valf() : top;
+    if constexpr (kBinned) {
+      if (searched) cut_room[threadIdx.x / TEAM % kTeams].clear(rank);  // (while the row is on its way)
+      team.most_and_least(top, low);
+    } else {
+      top = team.most(top);
+    }
     if (!(top < __builtin_huge_valf()) || top == kNone) {
       if (rank == 0) {
         a.actions[row] = -1;
@@ -829,12 +869,8 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(t
     float scale = 0.f;
     if constexpr (kBinned) {
       if (searched) {
-        low = team.all(low, [](float a, float b) { return a < b ? a : b; });
         const float range = __builtin_fminf(top - low, a.reach);
         scale = range > 0.f ? (float)CutRoom<TEAM>::kBins / range : 0.f;
-        CutRoom<TEAM>& m = cut_room[threadIdx.x / TEAM % kTeams];
-        m.clear(rank);
-        team.sync();
       }
     }
     double piece[R::PIECES], mine = 0., before, here, w[PER];
@@ -950,7 +986,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
   __shared__ double room[TEAM > 64 ? 2 * TEAM / 64 : 1];
   __shared__ double table[64], sums[kLossSums][team_block<TEAM>() / 64];
   Team<TEAM> team{room};
-  fill_powers(table, 1.);
+  fill_powers<TEAM>(table, 1.);
   constexpr int kTeams = team_block<TEAM>() / TEAM;
   double part[kLossSums] = {};
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
