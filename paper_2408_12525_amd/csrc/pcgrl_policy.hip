@@ -123,14 +123,39 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
   const bool cut = a.top_k > 0 || a.top_p < 1. || a.min_p > 0.;
   hipStream_t st = static_cast<hipStream_t>(stream);
   return by_type(how->type, [&](auto type) {
-    return by_classes(a.n, [&](auto shape) {
-      using T = decltype(type);
+    using T = decltype(type);
+    if (best) {
+      return by_classes(a.n, [&](auto shape) {
+        using S = decltype(shape);
+        hipLaunchKernelGGL((best_kernel<T, S::kTeam, S::kPer>), dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(team_block<S::kTeam>()), 0, st, a);
+        return launched();
+      });
+    }
+    auto few = [&](auto shape) {
       using S = decltype(shape);
-      auto* kernel = best ? &sample_kernel<T, S::kTeam, S::kPer, kSampleBest>
-                     : cut ? &sample_kernel<T, S::kTeam, S::kPer, kSampleCut> : &sample_kernel<T, S::kTeam, S::kPer, kSamplePlain>;
-      hipLaunchKernelGGL(kernel, dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(team_block<S::kTeam>()), 0, st, a);
+      hipLaunchKernelGGL((cut ? &sample_few_kernel<T, S::kTeam, S::kPer, kSampleCut> : &sample_few_kernel<T, S::kTeam, S::kPer, kSamplePlain>),
+                         dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(256), 0, st, a);
       return launched();
-    });
+    };
+    if (a.n <= 8) return few(Shape<1, 8>{});
+    if (a.n <= 64) return few(Shape<8, 8>{});
+    auto many = [&](auto shape) {
+      using S = decltype(shape);
+      constexpr int kVec = Stretch<T, S::kTeam>::VEC;
+      a.lds_row = (uint32_t)((a.n + 64 * kVec - 1) / (64 * kVec) * 1024);
+      const uint32_t lds = a.lds_row * (team_block<S::kTeam>() / S::kTeam);
+      auto* kernel = cut ? &sample_many_kernel<T, S::kTeam, kSampleCut> : &sample_many_kernel<T, S::kTeam, kSamplePlain>;
+      hipLaunchKernelGGL(kernel, dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(team_block<S::kTeam>()), lds, st, a);
+      return launched();
+    };
+    // A wavefront a row where it is short; a workgroup of 256 or 512 threads, of which a compute unit has room for more than one,
+    // or, for a few long rows, of 1024.  Measured, us for 64 / 256 / 512 / 1024 threads a row: 4096 rows of 1024 classes
+    // with top_p 22 / 41 / 80 / 184, 2000 of 4000 44 / 39 / 50 / 113, 1000 of 8000 - / 37 / 39 / 60, 1024 of 28 672 - / 148 / 103 / 135, 300 of
+    // 28 672 in float32 - / 118 / 72 / 59, one of 28 672 - / 50 / 35 / 31.
+    if (a.n <= 1024) return many(Shape<64, 1>{});
+    if (n_rows <= 384 && a.n > 4096) return many(Shape<1024, 1>{});
+    if (a.n <= 8192) return many(Shape<256, 1>{});
+    return many(Shape<512, 1>{});
   });
 }
 

@@ -233,6 +233,14 @@ __device__ __forceinline__ double power(const double* table, double z) {
   return __builtin_ldexp(__builtin_fma(of, q, of), n >> 6);
 }
 
+// The natural logarithm of v >= 1 (NaN for infinity and NaN), to about 2^-44, with `table` times 1 / `unit`: what the one in
+// single precision leaves, some 1e-7, by the series.  The library's takes a hundred registers of constants out of a loop.
+__device__ __forceinline__ double log_of(const double* table, double unit, double v) {
+  const double about = (double)__builtin_amdgcn_logf((float)v);
+  const double rest = v * (power(table, -64. * about) * (1. / unit)) - 1.;
+  return __builtin_fma(about, 0.69314718055994530942, rest - .5 * rest * rest);
+}
+
 // The classes of a thread: pieces of VEC neighbouring ones; each wavefront of a team has one stretch of the
 // row, in which its lanes' pieces lie side by side, so that running sums go from wavefront to wavefront.  The stretches are as
 // long as the row needs, to one piece, whatever the team could hold.  A piece is read at once, whatever its
@@ -342,30 +350,263 @@ struct SampleArgs {
   double slope;         // 64 * log2(e) / temperature
   float reach;          // below the largest logit by more than this there are no weights
   double inv_temperature, top_p, min_p;
+  uint32_t lds_row;     // bytes of LDS that a row takes
 };
 
 constexpr int kSampleBest = 0, kSamplePlain = 1, kSampleCut = 2;
 
-// Weights are held as whole numbers of 2^-bits in doubles, with as many bits as leave every sum of a row
-// below 2^53: sums are exact, whatever their order, so that a running sum cut up over lanes and wavefronts is the
-// same number as the sum of the parts.  (A weight is off by half a unit, at the most 2^-39 of the
-// largest one.)
-template <int CLASSES> constexpr double weight_unit() {
-  int bits = 53;
-  for (int c = 1; c < CLASSES; c <<= 1) --bits;
-  return (double)(1ll << bits);
-}
+// Weights are held as whole numbers of 2^-38 of the largest one in doubles: the sums of up to 2^15 of them stay below 2^53 and are
+// exact, whatever their order, so that a running sum cut up over lanes and wavefronts is the same number as the sum of the parts.
+constexpr double kUnit = 0x1p38;
 
 // The last of the classes that top_k and top_p keep, in the order of falling logits and rising indices.
-template <typename T, int TEAM, int PER> struct Held;
 struct Cutoff {
   uint32_t key;
   int index;
 };
 
-// LDS of a team that looks for it: weights and numbers of classes in bins of falling logits, and the classes of one bin.
+// How a row's weights follow from its logits.
+struct Weigh {
+  const double* table;
+  float top;
+  double slope;
+  __device__ __forceinline__ double operator()(float x) const { return __builtin_rint(power(table, ((double)x - (double)top) * slope)); }
+};
+// (the two zeros are equal)
+template <typename T> __device__ __forceinline__ uint32_t class_key(float x) { return key_of(x + 0.f) >> T::kKeyShift; }
+
+__device__ __forceinline__ void put_draw(const SampleArgs& a, int64_t row, int action, float logit, float top, double whole, const double* table) {
+  a.actions[row] = action;
+  if (a.log_probs) a.log_probs[row] = (float)(((double)logit - (double)top) * a.inv_temperature - log_of(table, kUnit, whole / kUnit));
+}
+__device__ __forceinline__ void put_nothing(const SampleArgs& a, int64_t row, float top) {
+  a.actions[row] = -1;
+  if (a.log_probs) a.log_probs[row] = top == kNone ? 0.f : __builtin_nanf("");
+}
+__device__ __forceinline__ double uniform_of(const SampleArgs& a, int64_t row) {
+  const double u = (double)a.uniform[row];
+  return u >= 0. ? u < 1. ? u : 1. - 0x1p-24 : 0.;
+}
+
+// The largest logit by itself, for any team.
+template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>()) void best_kernel(SampleArgs a) {
+  using R = Row<T, TEAM, PER>;
+  constexpr int kTeams = team_block<TEAM>() / TEAM;
+  __shared__ double room[TEAM > 64 ? 2 * TEAM / 64 : 1];
+  Team<TEAM> team{room};
+  for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
+    const int rank = team.rank_anew();
+    const R of(rank, a.n);
+    float x[PER], top = kNone;
+    of.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, x);
+    Oddity odd;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      top = __builtin_fmaxf(top, x[j]);
+      odd.look(x[j]);
+    }
+    top = team.most(odd.seen() ? __builtin_huge_valf() : top);
+    if (!(top < __builtin_huge_valf()) || top == kNone) {
+      if (rank == 0) put_nothing(a, row, top);
+      continue;
+    }
+    int best = a.n;
+#pragma unroll
+    for (int j = PER - 1; j >= 0; --j)
+      if (x[j] == top) best = of.at(j / R::VEC, j % R::VEC);
+    best = team.least(best);
+    if (rank == 0) {
+      a.actions[row] = best;
+      if (a.log_probs) a.log_probs[row] = 0.f;
+    }
+  }
+}
+
+// ---- few classes: a row in the registers of a lane or of eight
+
+// A lane that holds a whole row: each class against every other one.
+template <typename T, int PER> __device__ __forceinline__ Cutoff cut_lane(const float (&x)[PER], const double (&w)[PER], const SampleArgs& a) {
+  int before[PER];
+  double mass[PER], whole = 0.;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    before[j] = 0;
+    mass[j] = 0.;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (i == j) continue;
+      const bool first = x[i] > x[j] || (i < j && x[i] == x[j]);
+      before[j] += first;
+      mass[j] += first ? w[i] : 0.;
+    }
+  }
+  const int k = a.top_k > 0 ? a.top_k : PER;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) whole += before[j] < k ? w[j] : 0.;
+  const double share = a.top_p < 1. ? a.top_p * whole : __builtin_huge_val();
+  Cutoff cut{0, 0x7fffffff};
+  int most = -1;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const bool last = before[j] < k && mass[j] < share && before[j] > most;
+    most = last ? before[j] : most;
+    cut.key = last ? class_key<T>(x[j]) : cut.key;
+    cut.index = last ? j : cut.index;
+  }
+  return cut;
+}
+
+// By halving the range of keys, and where a key is kept in part that of the indices: a sum over the team for each bit.
+template <typename T, int TEAM, int PER>
+__device__ __forceinline__ Cutoff cut_by_halves(const float (&x)[PER], const double (&w)[PER], const Row<T, TEAM, PER>& of, Team<TEAM>& team, const SampleArgs& a,
+                                                double whole) {
+  using R = Row<T, TEAM, PER>;
+  constexpr int kBits = 32 - T::kKeyShift;
+  uint32_t key[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) key[j] = class_key<T>(x[j]);
+  auto count_from = [&](uint32_t k) {
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) c += key[j] >= k;
+    return team.sum(c);
+  };
+  auto sum_from = [&](uint32_t k) {
+    double s = 0.;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) s += key[j] >= k ? w[j] : 0.;
+    return team.sum(s);
+  };
+  auto weight_at = [&](uint32_t k) {  // of a class with this key
+    double v = 0.;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) v = key[j] == k ? w[j] : v;
+    return team.all(v, [](double a, double b) { return a > b ? a : b; });
+  };
+  uint32_t edge = 0;
+  int ties = 0x7fffffff;  // classes of the key `edge` that are kept
+  if (a.top_k > 0 && count_from(class_key<T>(kNone) + 1) > a.top_k) {
+#pragma unroll 1
+    for (int b = kBits - 1; b >= 0; --b) {
+      const uint32_t k = edge | (1u << b);
+      if (count_from(k) >= a.top_k) edge = k;
+    }
+    ties = a.top_k - count_from(edge + 1);
+    whole = sum_from(edge + 1) + ties * weight_at(edge);
+  }
+  if (a.top_p < 1.) {
+    const double share = a.top_p * whole;
+    uint32_t low = 0;
+#pragma unroll 1
+    for (int b = kBits - 1; b >= 0; --b) {
+      const uint32_t k = low | (1u << b);
+      if (sum_from(k) >= share) low = k;
+    }
+    // (not below `edge`: all of its classes together reach the share)
+    const double above = sum_from(low + 1), one = weight_at(low);
+    const int more = one > 0. ? (int)__builtin_fmin(__builtin_ceil((share - above) / one), (double)PCGRL_MAX_CLASSES) : 1;
+    ties = low == edge && ties < more ? ties : more;
+    edge = low;
+  }
+  auto count_until = [&](int until) {
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) c += key[j] == edge && of.at(j / R::VEC, j % R::VEC) <= until;
+    return team.sum(c);
+  };
+  Cutoff cut{edge, 0x7fffffff};
+  if (ties < PCGRL_MAX_CLASSES && count_until(a.n) > ties) {
+    int low = -1, high = a.n - 1;  // count_until(low) < ties <= count_until(high)
+    while (high - low > 1) {
+      const int mid = (low + high) >> 1;
+      if (count_until(mid) < ties) low = mid; else high = mid;
+    }
+    cut.index = high;
+  }
+  return cut;
+}
+
+template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(256) void sample_few_kernel(SampleArgs a) {
+  static_assert(TEAM <= 8 && HOW != kSampleBest, "");
+  using R = Row<T, TEAM, PER>;
+  constexpr int kTeams = 256 / TEAM;
+  __shared__ double table[64];
+  Team<TEAM> team{nullptr};
+  fill_powers<TEAM>(table, kUnit);
+  for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
+    const int rank = team.rank_anew();
+    const R of(rank, a.n);
+    float x[PER], top = kNone;
+    of.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, x);
+    Oddity odd;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      top = __builtin_fmaxf(top, x[j]);
+      odd.look(x[j]);
+    }
+    top = team.most(odd.seen() ? __builtin_huge_valf() : top);
+    if (!(top < __builtin_huge_valf()) || top == kNone) {
+      if (rank == 0) put_nothing(a, row, top);
+      continue;
+    }
+    const Weigh weigh{table, top, a.slope};
+    double w[PER], whole = 0.;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      w[j] = weigh(x[j]);
+      whole += w[j];
+    }
+    whole = team.sum(whole);
+    double kept = whole;
+    if constexpr (HOW == kSampleCut) {
+      Cutoff cut{0, 0x7fffffff};
+      if (a.top_k > 0 || a.top_p < 1.) {
+        if constexpr (TEAM == 1) cut = cut_lane<T, PER>(x, w, a);
+        else cut = cut_by_halves<T, TEAM, PER>(x, w, of, team, a, whole);
+      }
+      kept = 0.;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const uint32_t key = class_key<T>(x[j]);
+        w[j] = (key > cut.key || (key == cut.key && of.at(j / R::VEC, j % R::VEC) <= cut.index)) && w[j] >= a.min_p * kUnit ? w[j] : 0.;
+        kept += w[j];
+      }
+      kept = team.sum(kept);
+    }
+    // the first class whose running sum exceeds the target
+    const double target = uniform_of(a, row) * kept;
+    double before = 0.;
+#pragma unroll
+    for (int c = 0; c < R::PIECES; ++c) {
+      double piece = 0.;
+#pragma unroll
+      for (int e = 0; e < R::VEC; ++e) piece += w[c * R::VEC + e];
+      const double until = before + sum_until<TEAM>(piece);
+      double run = until - piece;
+      if (run <= target && target < until) {
+        int chosen = -1;
+        float logit = 0.f;
+#pragma unroll
+        for (int e = 0; e < R::VEC; ++e) {
+          run += w[c * R::VEC + e];
+          float v = x[c * R::VEC + e];
+          asm("" : "+v"(v));  // (else it becomes an address chosen among the classes, and they go to memory)
+          const bool it = chosen < 0 && run > target;
+          chosen = it ? of.at(c, e) : chosen;
+          logit = it ? v : logit;
+        }
+        put_draw(a, row, chosen, logit, top, whole, table);
+      }
+      if (c + 1 < R::PIECES) before = __shfl(until, TEAM - 1, TEAM);
+    }
+  }
+}
+
+// ---- many classes: a row in the LDS of a wavefront or a workgroup
+
+// LDS of a team that looks for a cutoff: weights and numbers of classes in bins of falling logits, and the classes of one bin.
 template <int TEAM> struct CutRoom {
-  static constexpr int kBins = TEAM == 64 ? 512 : 2048, kList = TEAM == 64 ? 128 : 512;
+  static constexpr int kBins = TEAM == 64 ? 256 : TEAM == 256 ? 512 : 1024, kList = TEAM == 64 ? 128 : 256;
   struct alignas(16) Entry {
     uint64_t order;  // the key, and below it the index turned round: what is kept first is larger
     double weight;
@@ -400,210 +641,107 @@ template <int TEAM> struct CutRoom {
     }
   }
   // of a class so far below the largest logit (a NaN, of 0 times infinity, goes to the last bin, with all others)
-  static __device__ int bin_of(float below, float scale) { return (int)__builtin_fminf(below * scale, (float)(kBins - 1)); }
+  static __device__ __forceinline__ int bin_of(float below, float scale) { return (int)__builtin_fminf(below * scale, (float)(kBins - 1)); }
 };
-template <> struct CutRoom<8> {};
-template <> struct CutRoom<1> {};
 
-// The classes of one thread.  Their weights are not held but computed again where they are needed: with them in registers a
-// workgroup of 1024 threads would have no room for its row.
-template <typename T, int TEAM, int PER> struct Held {
-  using R = Row<T, TEAM, PER>;
-  float x[PER];
-  R row;
-  float top;
-  __device__ __forceinline__ Held(int rank, int n) : row(rank, n) {}
-  __device__ __forceinline__ explicit Held(const R& r) : row(r) {}
-  double slope;
-  const double* table;
-  // (the two zeros are equal)
-  __device__ __forceinline__ uint32_t key(int j) const { return key_of(x[j] + 0.f) >> T::kKeyShift; }
-  __device__ __forceinline__ double weight(int j) const { return __builtin_rint(power(table, ((double)x[j] - (double)top) * slope)); }
-  __device__ __forceinline__ int at(int j) const { return row.at(j / R::VEC, j % R::VEC); }
-  // One of the pieces.
-  template <int VEC> __device__ __forceinline__ Held<T, TEAM, VEC> piece(int which) const {
-    Held<T, TEAM, VEC> p(0, VEC);  // (its row is not asked for)
-    p.top = top;
-    p.slope = slope;
-    p.table = table;
+// A row in LDS: each thread has written, and reads, its own pieces of it, of VEC neighbouring classes, so that no barrier is
+// needed; each wavefront has one stretch of the row, in which its lanes' pieces lie side by side, so that running sums go
+// from wavefront to wavefront.  What masks leave out, and what is behind the last class, is -infinity.
+template <typename T, int TEAM> struct Stretch {
+  using raw = typename T::raw;
+  static constexpr int VEC = 16 / (int)sizeof(raw), W = TEAM / 64;
+  raw* row;
+  int n, all, first, pieces;  // pieces of a row and of this wavefront (each of 64 lanes); this thread's first class
+  __device__ __forceinline__ Stretch(raw* lds, int rank, int classes) : row(lds), n(classes) {
+    all = (n + 64 * VEC - 1) / (64 * VEC);
+    const int w = __builtin_amdgcn_readfirstlane(rank >> 6), from = w * all / W;
+    pieces = (w + 1) * all / W - from;
+    first = (from * 64 + (rank & 63)) * VEC;
+  }
+  // the wavefront of a class: the last one that begins at its piece or before
+  __device__ __forceinline__ int wave_of(int index) const { return ((index / (64 * VEC) + 1) * W - 1) / all; }
+  // Reads the row, several pieces at a time, and shows every logit to `look`.
+  template <typename F> __device__ __forceinline__ void fill(const raw* from, const uint8_t* mask, F look) {
+    constexpr int kAtOnce = 4;
+#pragma unroll 1
+    for (int c0 = 0; c0 < pieces; c0 += kAtOnce) {
+      raw v[kAtOnce][VEC];
+      uint8_t m[kAtOnce][VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      float v = x[e];
-      asm("" : "+v"(v));
-#pragma unroll
-      for (int c = 1; c < PER / VEC; ++c) {
-        float o = x[c * VEC + e];
-        asm("" : "+v"(o));
-        v = which == c ? o : v;
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int b = first + (c0 + i) * 64 * VEC;
+        if (c0 + i < pieces && b + VEC <= n) {
+          __builtin_memcpy(v[i], from + b, sizeof(v[i]));
+          if (mask) __builtin_memcpy(m[i], mask + b, sizeof(m[i]));
+        }
       }
-      p.x[e] = v;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int b = first + (c0 + i) * 64 * VEC;
+        if (c0 + i >= pieces) break;
+        if (b + VEC <= n) {
+          if (mask) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[i][e] = m[i][e] == 0 ? T::store(kNone) : v[i][e];
+          }
+          __builtin_memcpy(__builtin_assume_aligned(row + b, 16), v[i], sizeof(v[i]));
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) look(T::load(v[i][e]));
+        } else {  // (behind the row, or the end of it)
+#pragma unroll 1
+          for (int e = 0; e < VEC; ++e) {
+            const raw r = b + e < n && (!mask || mask[b + e] != 0) ? from[b + e] : T::store(kNone);
+            row[b + e] = r;
+            look(T::load(r));
+          }
+        }
+      }
     }
-    return p;
   }
-  __device__ __forceinline__ void forget() { forget_classes<TEAM, PER>(x, row.first); }
+  template <typename F> __device__ __forceinline__ void piece(int c, F f) const {
+    raw v[VEC];
+    const int b = first + c * 64 * VEC;
+    __builtin_memcpy(v, __builtin_assume_aligned(row + b, 16), sizeof(v));
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f(T::load(v[e]), b + e);
+  }
+  // (four at a time, which are as many as there are registers for)
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+#pragma unroll 1
+    for (int q = 0; q < pieces * (VEC / 4); ++q) {
+      const int b = first + q / (VEC / 4) * 64 * VEC + q % (VEC / 4) * 4;
+      raw v[4];
+      __builtin_memcpy(v, __builtin_assume_aligned(row + b, 4 * sizeof(raw)), sizeof(v));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(T::load(v[e]), b + e);
+    }
+  }
+  // The class at which the running sum of `value` first exceeds `target`, in the wavefront that `before` and `here` say has it:
+  // calls `found` in its lane.
+  template <typename V, typename F> __device__ __forceinline__ void find(double before, double here, double target, V value, F found) const {
+    if (!(before <= target && target < before + here)) return;
+#pragma unroll 1
+    for (int c = 0; c < pieces; ++c) {
+      double sum = 0.;
+      piece(c, [&](float x, int index) { sum += value(x, index); });
+      const double until = before + sum_until<64>(sum);
+      double run = until - sum;
+      if (run <= target && target < until) {
+        int chosen = -1;
+        float logit = 0.f;
+        piece(c, [&](float x, int index) {
+          run += value(x, index);
+          const bool it = chosen < 0 && run > target;
+          chosen = it ? index : chosen;
+          logit = it ? x : logit;
+        });
+        found(chosen, logit);
+      }
+      before = of_lane(until, 63);
+      if (target < before) break;
+    }
+  }
 };
-template <typename T> __device__ __forceinline__ uint32_t no_key() { return key_of(kNone) >> T::kKeyShift; }
-
-// In the order of the classes, the one at which the running sum of `value` first exceeds `target`: calls `found` with it in the
-// lane that holds it.  `piece` has the sums of this thread's pieces, `before` that of the wavefronts before this
-// one, `here` that of this one.  All sums are exact, so that there is one such class if 0 <= target < the sum of all.
-template <typename T, int TEAM, int PER, typename V, typename F>
-__device__ __forceinline__ void find_class(const Held<T, TEAM, PER>& h, const double (&piece)[Row<T, TEAM, PER>::PIECES], double before, double here, double target,
-                                           V value, F found) {
-  using R = Row<T, TEAM, PER>;
-  if (R::LANES == 64 && !(before <= target && target < before + here)) return;
-  // the piece, and its classes
-  double sum = 0., until = 0.;
-  int which = 0;
-#pragma unroll
-  for (int c = 0; c < R::PIECES; ++c) {
-    const double all = over_lanes<R::LANES>(piece[c], [](double a, double b) { return a + b; });
-    const bool it = c == 0 || !(target < before);
-    which = it ? c : which;
-    sum = it ? piece[c] : sum;
-    until = it ? before : until;
-    before += all;
-  }
-  Held<T, TEAM, R::VEC> in = h.template piece<R::VEC>(which);
-  until += sum_until<R::LANES>(sum);
-  double run = until - sum;
-  if (run <= target && target < until) {
-    int at = -1;
-    float logit = 0.f;
-#pragma unroll
-    for (int e = 0; e < R::VEC; ++e) {
-      const int index = h.row.at(which, e);
-      run += value(in, e, index);
-      float x = in.x[e];
-      asm("" : "+v"(x));  // (else it becomes an address chosen among the classes, and they go to memory)
-      const bool it = at < 0 && run > target;
-      at = it ? index : at;
-      logit = it ? x : logit;
-    }
-    found(at, logit);
-  }
-}
-
-// A lane that holds a whole row: each class against every other one.
-template <typename T, int PER> __device__ __forceinline__ Cutoff cut_lane(const Held<T, 1, PER>& h, const SampleArgs& a, const double (&w)[PER]) {
-  int before[PER];
-  double mass[PER], whole = 0.;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    before[j] = 0;
-    mass[j] = 0.;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      if (i == j) continue;
-      const bool first = h.x[i] > h.x[j] || (i < j && h.x[i] == h.x[j]);
-      before[j] += first;
-      mass[j] += first ? w[i] : 0.;
-    }
-  }
-  const int k = a.top_k > 0 ? a.top_k : PER;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) whole += before[j] < k ? w[j] : 0.;
-  const double share = a.top_p < 1. ? a.top_p * whole : __builtin_huge_val();
-  Cutoff cut{0, 0x7fffffff};
-  int most = -1;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const bool last = before[j] < k && mass[j] < share && before[j] > most;
-    most = last ? before[j] : most;
-    cut.key = last ? h.key(j) : cut.key;
-    cut.index = last ? j : cut.index;
-  }
-  return cut;
-}
-
-// The last of the first `ties` classes of the key `key`, by index.
-template <typename T, int TEAM, int PER> __device__ __forceinline__ Cutoff cut_ties(Held<T, TEAM, PER>& h, Team<TEAM>& team, uint32_t key, int ties, Cutoff* shared) {
-  using R = Row<T, TEAM, PER>;
-  double piece[R::PIECES], mine = 0., before, here;
-  h.forget();
-#pragma unroll
-  for (int c = 0; c < R::PIECES; ++c) {
-    piece[c] = 0.;
-#pragma unroll
-    for (int e = 0; e < R::VEC; ++e) piece[c] += h.key(c * R::VEC + e) == key ? 1. : 0.;
-    mine += piece[c];
-  }
-  Cutoff cut{key, 0x7fffffff};
-  if (team.sum(mine, before, here) > (double)ties) {
-    int last = 0x7fffffff;
-    find_class(h, piece, before, here, (double)(ties - 1), [&](const Held<T, TEAM, R::VEC>& in, int e, int) { return in.key(e) == key ? 1. : 0.; },
-               [&](int at, float) { last = at; });
-    if constexpr (TEAM > 64) {
-      if (last != 0x7fffffff) shared->index = last;
-      team.sync();
-      last = shared->index;
-      team.sync();
-    } else {
-      last = team.least(last);
-    }
-    cut.index = last;
-  }
-  return cut;
-}
-
-// By halving the range of keys: a sum over the team for each bit.
-template <typename T, int TEAM, int PER>
-__device__ __forceinline__ Cutoff cut_by_halves(Held<T, TEAM, PER>& h, Team<TEAM>& team, const SampleArgs& a, double whole, Cutoff* shared) {
-  constexpr int kBits = 32 - T::kKeyShift;
-  auto count_from = [&](uint32_t k) {
-    int c = 0;
-    h.forget();
-#pragma unroll
-    for (int j = 0; j < PER; ++j) c += h.key(j) >= k;
-    return team.sum(c);
-  };
-  auto sum_from = [&](uint32_t k) {
-    double s = 0.;
-    h.forget();
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      s += h.key(j) >= k ? h.weight(j) : 0.;
-      part_end(j, s);
-    }
-    return team.sum(s);
-  };
-  auto weight_at = [&](uint32_t k) {  // of a class with this key
-    double v = 0.;
-    h.forget();
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      v = h.key(j) == k ? h.weight(j) : v;
-      part_end(j, v);
-    }
-    return team.all(v, [](double a, double b) { return a > b ? a : b; });
-  };
-  uint32_t edge = 0;
-  int ties = 0x7fffffff;  // classes of the key `edge` that are kept
-  if (a.top_k > 0 && count_from(no_key<T>() + 1) > a.top_k) {
-#pragma unroll 1
-    for (int b = kBits - 1; b >= 0; --b) {
-      const uint32_t k = edge | (1u << b);
-      if (count_from(k) >= a.top_k) edge = k;
-    }
-    ties = a.top_k - count_from(edge + 1);
-    whole = sum_from(edge + 1) + ties * weight_at(edge);
-  }
-  if (a.top_p < 1.) {
-    const double share = a.top_p * whole;
-    uint32_t low = 0;
-#pragma unroll 1
-    for (int b = kBits - 1; b >= 0; --b) {
-      const uint32_t k = low | (1u << b);
-      if (sum_from(k) >= share) low = k;
-    }
-    // (not below `edge`: all of its classes together reach the share)
-    const double above = sum_from(low + 1), one = weight_at(low);
-    const int more = one > 0. ? (int)__builtin_fmin(__builtin_ceil((share - above) / one), (double)PCGRL_MAX_CLASSES) : 1;
-    ties = low == edge && ties < more ? ties : more;
-    edge = low;
-  }
-  return cut_ties<T, TEAM, PER>(h, team, edge, ties, shared);
-}
 
 // The sums before a thread's bins.
 template <int TEAM> struct BinSums {
@@ -630,10 +768,13 @@ template <int TEAM> struct BinSums {
       team.sync();
       double behind = 0.;
       int passed = 0;
+#pragma unroll
       for (int i = 0; i < TEAM / 64; ++i) {
         behind += i < wave ? m.wave_mass[i] : 0.;
-        passed += i < wave ? m.wave_count[i] : 0;
-        all += m.wave_count[i];
+        if (counted) {
+          passed += i < wave ? m.wave_count[i] : 0;
+          all += m.wave_count[i];
+        }
       }
       run += behind;
       seen += passed;
@@ -648,40 +789,39 @@ template <int TEAM> struct BinSums {
 // By bins: the weights (for top_k the numbers) of a row's classes are added up in LDS in bins of equal width from the
 // largest logit down to the smallest one, or to where weights vanish; the bin in which the sum from the
 // top reaches what is looked for is listed, and each of its few classes is ranked against the others.  Three passes over the
-// row in registers, whatever the types.  A bin with more classes than the list holds is binned again by itself, unless they are
+// row, whatever the types.  A bin with more classes than the list holds is binned again by itself, unless they are
 // all equal: then they are counted off by index.
-template <typename T, int TEAM, int PER>
-__device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double whole, float low, float scale) {
+template <typename T, int TEAM>
+__device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const Weigh& weigh, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double whole,
+                                              float low, float scale) {
   using C = CutRoom<TEAM>;
   constexpr int kOwn = C::kBins / TEAM;
   const int rank = Team<TEAM>::rank();
   Cutoff cut{0, 0x7fffffff};
   bool by_mass = a.top_k == 0;
-  float from = h.top, to = low, by = scale;  // the logits that are binned, and how
-  double mass_before = 0.;                   // of the logits above them
+  float from = weigh.top, to = low, by = scale;  // the logits that are binned, and how
+  double mass_before = 0.;                       // of the logits above them
   int count_before = 0;
+  auto inside = [&](float x) { return x <= from && x >= to && x != kNone; };
 #pragma unroll 1
   for (bool binned = true;; binned = false) {
     if (!binned) {
       team.sync();
       m.clear(rank);
       team.sync();
-      h.forget();
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        if (h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone) {
-          const int b = C::bin_of(from - h.x[j], by);
-          unsafeAtomicAdd(&m.mass[b], h.weight(j));
+      in.each([&](float x, int) {
+        if (inside(x)) {
+          const int b = C::bin_of(from - x, by);
+          unsafeAtomicAdd(&m.mass[b], weigh(x));
           if (a.top_k > 0) atomicAdd(&m.count[b], 1);
         }
-      }
+      });
       team.sync();
     }
     const BinSums<TEAM> sums(team, m, rank, a.top_k > 0);
-    const int all = sums.all;
     double run = sums.run + mass_before;
     int seen = sums.seen + count_before;
-    if (!by_mass && binned && all <= a.top_k) by_mass = true;  // top_k keeps all
+    if (!by_mass && binned && sums.all <= a.top_k) by_mass = true;  // top_k keeps all
     if (by_mass && !(a.top_p < 1.)) break;
     const double share = a.top_p * whole;
 #pragma unroll
@@ -700,35 +840,38 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
     }
     team.sync();
     const int bin = m.bin;
-    h.forget();
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      if (!h.row.has(j / Held<T, TEAM, PER>::R::VEC)) continue;
-      if (h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone && C::bin_of(from - h.x[j], by) == bin) {
-        m.put(h.key(j), h.at(j), h.weight(j));
-      }
-    }
+    in.each([&](float x, int index) {
+      if (inside(x) && C::bin_of(from - x, by) == bin) m.put(class_key<T>(x), index, weigh(x));
+    });
     team.sync();
     const int listed = m.listed;
     mass_before = m.mass_before;
     count_before = m.count_before;
     if (listed > C::kList) {
       float most = kNone, least = -kNone;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const bool in = h.x[j] <= from && h.x[j] >= to && h.x[j] != kNone && C::bin_of(from - h.x[j], by) == bin;
-        most = in && h.x[j] > most ? h.x[j] : most;
-        least = in && h.x[j] < least ? h.x[j] : least;
-      }
-      from = team.most(most);
-      to = team.all(least, [](float a, float b) { return a < b ? a : b; });
+      in.each([&](float x, int) {
+        if (inside(x) && C::bin_of(from - x, by) == bin) {
+          most = __builtin_fmaxf(most, x);
+          least = __builtin_fminf(least, x);
+        }
+      });
+      team.most_and_least(most, least);
+      from = most;
+      to = least;
       if (to < from) {
         by = (float)C::kBins / (from - to);
         continue;
       }
+      // all equal: the first few by index, as many as it takes
       const double one = m.list[0].weight;
       const int ties = by_mass ? (int)__builtin_fmin(__builtin_ceil((share - mass_before) / one), (double)PCGRL_MAX_CLASSES) : a.top_k - count_before;
-      cut = cut_ties<T, TEAM, PER>(h, team, C::cutoff(m.list[0].order).key, ties, &m.found);
+      auto equal = [&](float x, int) { return x == from ? 1. : 0.; };
+      double mine = 0., before, here;
+      in.each([&](float x, int index) { mine += equal(x, index); });
+      team.sum(mine, before, here);
+      in.find(before, here, (double)(ties - 1), equal, [&](int index, float x) { m.found = Cutoff{class_key<T>(x), index}; });
+      team.sync();
+      cut = m.found;
       whole = mass_before + (double)ties * one;
     } else {
       for (int i = rank; i < listed; i += TEAM) {
@@ -748,7 +891,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
     }
     if (by_mass || !(a.top_p < 1.)) break;
     by_mass = true;  // top_p, of what top_k has left
-    from = h.top;
+    from = weigh.top;
     to = low;
     by = scale;
     mass_before = 0.;
@@ -760,10 +903,10 @@ __device__ __forceinline__ Cutoff cut_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
 // The same for top_p alone, which has the classes of the bins above added up in the pass that lists the bin: sets `mine` to what
 // of this thread's classes is kept outside that bin, m.extra to what each wavefront has in it.  False if the list does not
 // hold the bin.
-template <typename T, int TEAM, int PER>
-__device__ __forceinline__ bool share_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>& team, CutRoom<TEAM>& m, double share, double least, float scale, double& mine) {
+template <typename T, int TEAM>
+__device__ __forceinline__ bool share_by_bins(const Stretch<T, TEAM>& in, const Weigh& weigh, Team<TEAM>& team, CutRoom<TEAM>& m, double share, double least, float scale,
+                                              double& mine) {
   using C = CutRoom<TEAM>;
-  using R = Row<T, TEAM, PER>;
   constexpr int kOwn = C::kBins / TEAM;
   const int rank = Team<TEAM>::rank();
   const BinSums<TEAM> sums(team, m, rank, false);
@@ -781,22 +924,13 @@ __device__ __forceinline__ bool share_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
   if (rank < TEAM / 64) m.extra[rank] = 0.;
   team.sync();
   const int bin = m.bin;
-  h.forget();
   mine = 0.;
-#pragma unroll
-  for (int c = 0; c < R::PIECES; ++c) {
-    if (!h.row.has(c)) continue;
-#pragma unroll
-    for (int e = 0; e < R::VEC; ++e) {
-      const int j = c * R::VEC + e, b = C::bin_of(h.top - h.x[j], scale);
-      const double w = h.weight(j);
-      mine += b < bin && w >= least ? w : 0.;
-      if (b == bin && h.x[j] != kNone) {
-        m.put(h.key(j), h.at(j), w);
-      }
-      part_end(j, mine);
-    }
-  }
+  in.each([&](float x, int index) {
+    const int b = C::bin_of(weigh.top - x, scale);
+    const double w = weigh(x);
+    mine += b < bin && w >= least ? w : 0.;
+    if (b == bin && x != kNone) m.put(class_key<T>(x), index, w);
+  });
   team.sync();
   const int listed = m.listed;
   if (listed > C::kList) return false;
@@ -808,151 +942,91 @@ __device__ __forceinline__ bool share_by_bins(Held<T, TEAM, PER>& h, Team<TEAM>&
     if (before < share) {
       const Cutoff it = C::cutoff(e.order);
       if (share <= before + e.weight) m.found = it;
-      if (e.weight >= least) unsafeAtomicAdd(&m.extra[h.row.wave_of(it.index)], e.weight);
+      if (e.weight >= least) unsafeAtomicAdd(&m.extra[in.wave_of(it.index)], e.weight);
     }
   }
   team.sync();
   return true;
 }
 
-template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), team_waves<TEAM>()) void sample_kernel(SampleArgs a) {
-  using R = Row<T, TEAM, PER>;
+template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), team_waves<TEAM>()) void sample_many_kernel(SampleArgs a) {
+  static_assert(TEAM >= 64 && HOW != kSampleBest, "");
+  using S = Stretch<T, TEAM>;
   constexpr int kTeams = team_block<TEAM>() / TEAM;
-  constexpr double kUnit = weight_unit<TEAM * PER>();
-  constexpr bool kBinned = HOW == kSampleCut && TEAM >= 64;
+  extern __shared__ char rows_lds[];
   __shared__ double table[64], room[TEAM > 64 ? 2 * TEAM / 64 : 1];
-  __shared__ CutRoom<kBinned ? TEAM : 1> cut_room[kBinned ? kTeams : 1];
+  __shared__ CutRoom<TEAM> cut_room[HOW == kSampleCut ? kTeams : 1];
   Team<TEAM> team{room};
-  if (HOW != kSampleBest) fill_powers<TEAM>(table, kUnit);
+  CutRoom<TEAM>& m = cut_room[HOW == kSampleCut ? threadIdx.x / TEAM % kTeams : 0];
+  fill_powers<TEAM>(table, kUnit);
   const bool searched = HOW == kSampleCut && (a.top_k > 0 || a.top_p < 1.);
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
     const int rank = team.rank_anew();
-    Held<T, TEAM, PER> h(rank, a.n);
-    h.row.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, h.x);
+    S in(reinterpret_cast<typename T::raw*>(rows_lds + (size_t)(threadIdx.x / TEAM % kTeams) * a.lds_row), rank, a.n);
     float top = kNone, low = -kNone;
     Oddity odd;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      top = __builtin_fmaxf(top, h.x[j]);
-      if (kBinned) low = __builtin_fminf(low, h.x[j] == kNone ? -kNone : h.x[j]);
-      odd.look(h.x[j]);
-    }
+    in.fill(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, [&](float x) {
+      top = __builtin_fmaxf(top, x);
+      if (HOW == kSampleCut) low = __builtin_fminf(low, x == kNone ? -kNone : x);
+      odd.look(x);
+    });
     top = odd.seen() ? __builtin_huge_valf() : top;
-    if constexpr (kBinned) {
-      if (searched) cut_room[threadIdx.x / TEAM % kTeams].clear(rank);  // (while the row is on its way)
+    if constexpr (HOW == kSampleCut) {
+      if (searched) m.clear(rank);
       team.most_and_least(top, low);
     } else {
       top = team.most(top);
     }
     if (!(top < __builtin_huge_valf()) || top == kNone) {
-      if (rank == 0) {
-        a.actions[row] = -1;
-        if (a.log_probs) a.log_probs[row] = top == kNone ? 0.f : __builtin_nanf("");
-      }
+      if (rank == 0) put_nothing(a, row, top);
       continue;
     }
-    if constexpr (HOW == kSampleBest) {
-      int best = a.n;
-#pragma unroll
-      for (int j = PER - 1; j >= 0; --j)
-        if (h.x[j] == top) best = h.at(j);
-      best = team.least(best);
-      if (rank == 0) {
-        a.actions[row] = best;
-        if (a.log_probs) a.log_probs[row] = 0.f;
+    const Weigh weigh{table, top, a.slope};
+    const float range = __builtin_fminf(top - low, a.reach), scale = HOW == kSampleCut && range > 0.f ? (float)CutRoom<TEAM>::kBins / range : 0.f;
+    double mine = 0., before, here;
+    in.each([&](float x, int) {
+      const double w = weigh(x);
+      mine += w;
+      if (HOW == kSampleCut && searched) {
+        const int b = m.bin_of(top - x, scale);
+        if (w > 0.) unsafeAtomicAdd(&m.mass[b], w);
+        if (a.top_k > 0 && x != kNone) atomicAdd(&m.count[b], 1);
       }
-      continue;
-    }
-    h.top = top;
-    h.slope = a.slope;
-    h.table = table;
-    float scale = 0.f;
-    if constexpr (kBinned) {
-      if (searched) {
-        const float range = __builtin_fminf(top - low, a.reach);
-        scale = range > 0.f ? (float)CutRoom<TEAM>::kBins / range : 0.f;
-      }
-    }
-    double piece[R::PIECES], mine = 0., before, here, w[PER];
-    h.forget();
-#pragma unroll
-    for (int c = 0; c < R::PIECES; ++c) {
-      piece[c] = 0.;
-      if (!h.row.has(c)) continue;
-#pragma unroll
-      for (int e = 0; e < R::VEC; ++e) {
-        const int j = c * R::VEC + e;
-        w[j] = h.weight(j);
-        piece[c] += w[j];
-        if constexpr (kBinned) {
-          if (searched) {
-            CutRoom<TEAM>& m = cut_room[threadIdx.x / TEAM % kTeams];
-            const int b = m.bin_of(top - h.x[j], scale);
-            if (w[j] > 0.) unsafeAtomicAdd(&m.mass[b], w[j]);
-            if (a.top_k > 0 && h.x[j] != kNone) atomicAdd(&m.count[b], 1);
-          }
-        }
-        part_end(j, piece[c]);
-      }
-      mine += piece[c];
-    }
+    });
     const double whole = team.sum(mine, before, here);
     double kept = whole;
     const double least = HOW == kSampleCut ? a.min_p * kUnit : 0.;
     Cutoff cut{0, 0x7fffffff};
     // what is kept of a class's weight
-    auto kept_of = [&](const auto& in, int j, int index) {
-      const double v = in.weight(j);
-      const uint32_t key = in.key(j);
+    auto kept_of = [&](float x, int index) {
+      const double v = weigh(x);
+      const uint32_t key = class_key<T>(x);
       return HOW != kSampleCut || ((key > cut.key || (key == cut.key && index <= cut.index)) && v >= least) ? v : 0.;
     };
-    double u = (double)a.uniform[row];
-    u = u >= 0. ? u : 0.;
-    u = u < 1. ? u : 1. - 0x1p-24;
     if constexpr (HOW == kSampleCut) {
-      bool summed = false;  // what is kept, for each wavefront
-      if constexpr (kBinned) {
-        if (searched) {
-          CutRoom<TEAM>& m = cut_room[threadIdx.x / TEAM % kTeams];
-          if (TEAM == 64) team.sync();
-          if (a.top_k == 0) {
-            summed = share_by_bins<T, TEAM, PER>(h, team, m, a.top_p * whole, least, scale, mine);
-            if (summed) {
-              cut = m.found;
-              kept = team.sum(mine, before, here, m.extra);
-            }
+      bool summed = false;
+      if (searched) {
+        if (TEAM == 64) team.sync();
+        if (a.top_k == 0) {
+          summed = share_by_bins<T, TEAM>(in, weigh, team, m, a.top_p * whole, least, scale, mine);
+          if (summed) {
+            cut = m.found;
+            kept = team.sum(mine, before, here, m.extra);
           }
-          if (!summed) cut = cut_by_bins<T, TEAM, PER>(h, team, a, m, whole, low, scale);
         }
-      } else if constexpr (TEAM > 1) {
-        if (searched) cut = cut_by_halves<T, TEAM, PER>(h, team, a, whole, nullptr);
-      } else {
-        cut = cut_lane<T, PER>(h, a, w);
+        if (!summed) cut = cut_by_bins<T, TEAM>(in, weigh, team, a, m, whole, low, scale);
       }
-      // for each piece: in all wavefronts, or in the one where the running sum exceeds the target
-      if (!summed || (before <= u * kept && u * kept < before + here)) {
-        h.forget();
+      if (!summed) {
         mine = 0.;
-#pragma unroll
-        for (int c = 0; c < R::PIECES; ++c) {
-          piece[c] = 0.;
-          if (!h.row.has(c)) continue;
-#pragma unroll
-          for (int e = 0; e < R::VEC; ++e) {
-            piece[c] += kept_of(h, c * R::VEC + e, h.row.at(c, e));
-            part_end(c * R::VEC + e, piece[c]);
-          }
-          mine += piece[c];
-        }
+        in.each([&](float x, int index) {
+          const uint32_t key = class_key<T>(x);  // (top_k may leave none in most places)
+          if (__builtin_amdgcn_ballot_w64(key >= cut.key) != 0) mine += kept_of(x, index);
+        });
+        kept = team.sum(mine, before, here);
       }
-      if (!summed) kept = team.sum(mine, before, here);
     }
-    const double target = u * kept;
-    h.forget();
-    find_class(h, piece, before, here, target, kept_of, [&](int at, float logit) {
-      a.actions[row] = at;
-      if (a.log_probs) a.log_probs[row] = (float)(((double)logit - (double)top) * a.inv_temperature - log(whole / kUnit));
-    });
+    in.find(before, here, uniform_of(a, row) * kept, kept_of, [&](int index, float logit) { put_draw(a, row, index, logit, top, whole, table); });
+    if (TEAM > 64 && HOW == kSampleCut) team.sync();  // (the next row's bins are cleared before its first barrier)
   }
 }
 
@@ -1028,7 +1102,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     }
     whole = top < __builtin_huge_valf() ? team.sum(whole) : __builtin_nan("");
     spread = team.sum(spread);
-    const double log_whole = log(whole);
+    const double log_whole = log_of(table, 1., whole);
     const double entropy = log_whole - 0.69314718055994530942 / 64. * (spread / whole);
     const double logp = ((double)mine - (double)top) * a.inv_temperature - log_whole;
     double pull = 0.;                     // the policy loss's derivative by the log-probability
