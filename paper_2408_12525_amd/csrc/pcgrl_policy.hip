@@ -37,9 +37,13 @@ template <typename F> int by_type(int type, F&& f) {
   return f(BF16{});
 }
 template <typename F> int by_classes(int n, F&& f) {
+  if (n <= 2) return f(Shape<1, 2>{});
+  if (n <= 4) return f(Shape<1, 4>{});
   if (n <= 8) return f(Shape<1, 8>{});
   if (n <= 64) return f(Shape<8, 8>{});
-  if (n <= 512) return f(Shape<64, 8>{});
+  if (n <= 128) return f(Shape<8, 16>{});
+  if (n <= 256) return f(Shape<16, 16>{});
+  if (n <= 512) return f(Shape<16, 32>{});
   if (n <= 1024) return f(Shape<64, 16>{});
   if (n <= 2048) return f(Shape<256, 8>{});
   if (n <= 4096) return f(Shape<256, 16>{});
@@ -137,6 +141,8 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
                          dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(256), 0, st, a);
       return launched();
     };
+    if (a.n <= 2) return few(Shape<1, 2>{});
+    if (a.n <= 4) return few(Shape<1, 4>{});
     if (a.n <= 8) return few(Shape<1, 8>{});
     if (a.n <= 64) return few(Shape<8, 8>{});
     auto many = [&](auto shape) {
@@ -155,6 +161,7 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
     if (a.n <= 1024) return many(Shape<64, 1>{});
     if (n_rows <= 384 && a.n > 4096) return many(Shape<1024, 1>{});
     if (a.n <= 8192) return many(Shape<256, 1>{});
+    if (a.n * (int)sizeof(typename T::raw) > 61440) return many(Shape<1024, 1>{});  // (one row is as much LDS as there is)
     return many(Shape<512, 1>{});
   });
 }

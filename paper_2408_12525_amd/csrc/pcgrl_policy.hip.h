@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 // Lets the compiler forget what it has computed from the classes of a thread: what it would keep from one pass over them to
 // the next takes more registers than there are.
 template <int TEAM, int PER> __device__ __forceinline__ void forget_classes(float (&x)[PER], int& first) {
-  if constexpr (TEAM >= 64) {
+  if constexpr (PER >= 16 || TEAM >= 64) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) asm volatile("" : "+v"(x[j]));
     asm volatile("" : "+v"(first));
@@ -81,14 +81,14 @@ __device__ __forceinline__ double of_lane(double v, int lane) { return __hiloint
 
 // op over the first LANES lanes of every LANES, in all of them.
 template <int LANES, typename V, typename Op> __device__ __forceinline__ V over_lanes(V v, Op op) {
-  static_assert(LANES == 1 || LANES == 8 || LANES == 64, "");
+  static_assert(LANES == 1 || LANES == 8 || LANES == 16 || LANES == 64, "");
   if constexpr (LANES >= 8) {
     v = op(v, moved<0xB1>(v));   // the other of a pair
     v = op(v, moved<0x4E>(v));   // the other pair of four
     v = op(v, moved<0x141>(v));  // the other four of eight
   }
+  if constexpr (LANES >= 16) v = op(v, moved<0x140>(v));  // the other eight of sixteen
   if constexpr (LANES == 64) {
-    v = op(v, moved<0x140>(v));  // the other eight of sixteen
     v = op(op(of_lane(v, 0), of_lane(v, 16)), op(of_lane(v, 32), of_lane(v, 48)));
   }
   return v;
@@ -189,6 +189,22 @@ template <int TEAM> struct Team {
     }
     return here;
   }
+  __device__ __forceinline__ void sum_both(double& v, double& w) {
+    v = over_lanes<kLanes>(v, [](double a, double b) { return a + b; });
+    w = over_lanes<kLanes>(w, [](double a, double b) { return a + b; });
+    if constexpr (TEAM > 64) {  // (with room for two doubles a wavefront in each of the two sets)
+      double2* at = reinterpret_cast<double2*>(room) + turn * kWaves;
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = double2{v, w};
+      __syncthreads();
+      v = w = 0.;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        v += at[i].x;
+        w += at[i].y;
+      }
+    }
+  }
   __device__ int least(int v) {
     return all(v, [](int a, int b) { return a < b ? a : b; });
   }
@@ -276,27 +292,34 @@ template <typename T, int TEAM, int PER> struct Row {
     const int b = begin(c);
     return (TEAM > 1 && b > n - VEC ? n - VEC : b) + e;
   }
-  // Logits of the classes that may be chosen, kNone for the others.
-  __device__ __forceinline__ void load(const typename T::raw* row, const uint8_t* mask, float (&x)[PER]) const {
+  // Logits of the classes that may be chosen, kNone for the others.  For a lane that holds a row, `ahead` and `mask_ahead` are the
+  // elements from the row's first to the end of all rows: where there are as many as the lane could hold, it reads so many
+  // at once, the next row's first ones among them, and not each class by itself.
+  __device__ __forceinline__ void load(const typename T::raw* row, const uint8_t* mask, int64_t ahead, int64_t mask_ahead, float (&x)[PER]) const {
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) {
       const int b = begin(c), from = TEAM > 1 && b > n - VEC ? n - VEC : b;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[c * VEC + e] = kNone;
-      if (has(c) && (TEAM > 1 ? b < n : b + VEC <= n)) {
+      if (TEAM > 1 ? has(c) && b < n : b < n && ahead >= PER) {
         typename T::raw v[VEC];
         __builtin_memcpy(v, row + from, sizeof(v));
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x[c * VEC + e] = T::load(v[e]);
         if (mask) {
           uint8_t m[VEC];
-          __builtin_memcpy(m, mask + from, sizeof(m));
+          if (TEAM > 1 || mask_ahead >= PER) {
+            __builtin_memcpy(m, mask + from, sizeof(m));
+          } else {  // (the last rows, and one row for all)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) m[e] = b + e < n ? mask[b + e] : 0;
+          }
 #pragma unroll
           for (int e = 0; e < VEC; ++e) x[c * VEC + e] = m[e] == 0 ? kNone : x[c * VEC + e];
         }
-        if (TEAM > 1 && from < b) {
+        if (TEAM > 1 ? from < b : b + VEC > n) {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) x[c * VEC + e] = from + e < b ? kNone : x[c * VEC + e];
+          for (int e = 0; e < VEC; ++e) x[c * VEC + e] = (TEAM > 1 ? from + e < b : b + e >= n) ? kNone : x[c * VEC + e];
         }
       } else if (TEAM == 1) {
 #pragma unroll
@@ -315,9 +338,25 @@ template <typename T, int TEAM, int PER> struct Row {
     if (b + VEC <= n) {
       __builtin_memcpy(row + b, v, sizeof(v));
     } else if (b < n) {
+      if constexpr (TEAM == 1) {  // four, two and one of them
+        constexpr int kSize = sizeof(typename T::raw);
+        const int left = n - b;
+        if (VEC > 4 && left & 4) __builtin_memcpy(row + b, v, 4 * kSize);
+        if (left & 2) {
+          if (VEC > 4 && left & 4) __builtin_memcpy(row + b + 4, v + 4 % VEC, 2 * kSize);
+          else __builtin_memcpy(row + b, v, 2 * kSize);
+        }
+        if (left & 1) {
+          typename T::raw last = v[0];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (from + e >= b && from + e < n) row[from + e] = v[e];
+          for (int e = 2; e < VEC; e += 2) last = left - 1 == e ? v[e] : last;
+          row[n - 1] = last;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (from + e >= b) row[from + e] = v[e];
+      }
     }
   }
 };
@@ -332,10 +371,10 @@ template <typename... V> __device__ __forceinline__ void part_end(int j, V&... s
   }
 }
 
-// Wavefronts that a SIMD has room for at least: two workgroups of 512 threads a compute unit, one of which waits for its rows
-// while the other computes.
-template <int TEAM> constexpr int team_waves() { return TEAM >= 64 ? 4 : 1; }
 template <int TEAM> constexpr int team_block() { return TEAM > 64 ? TEAM : 256; }
+
+// Elements from row `row` to the end of `rows` rows of n.
+__device__ __forceinline__ int64_t from_row(int64_t row, int64_t rows, int64_t stride, int n) { return (rows - 1 - row) * stride + n; }
 
 // ---- actions drawn from logits
 
@@ -398,7 +437,8 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     const int rank = team.rank_anew();
     const R of(rank, a.n);
     float x[PER], top = kNone;
-    of.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, x);
+    of.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr,
+            from_row(row, a.n_rows, a.logits_stride, a.n), from_row(row, a.n_rows, a.mask_stride, a.n), x);
     Oddity odd;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -537,7 +577,8 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(2
     const int rank = team.rank_anew();
     const R of(rank, a.n);
     float x[PER], top = kNone;
-    of.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr, x);
+    of.load(static_cast<const typename T::raw*>(a.logits) + row * a.logits_stride, a.mask ? a.mask + row * a.mask_stride : nullptr,
+            from_row(row, a.n_rows, a.logits_stride, a.n), from_row(row, a.n_rows, a.mask_stride, a.n), x);
     Oddity odd;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -949,7 +990,7 @@ __device__ __forceinline__ bool share_by_bins(const Stretch<T, TEAM>& in, const 
   return true;
 }
 
-template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), team_waves<TEAM>()) void sample_many_kernel(SampleArgs a) {
+template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), 4) void sample_many_kernel(SampleArgs a) {
   static_assert(TEAM >= 64 && HOW != kSampleBest, "");
   using S = Stretch<T, TEAM>;
   constexpr int kTeams = team_block<TEAM>() / TEAM;
@@ -1054,11 +1095,11 @@ struct LossArgs {
 constexpr int kLossSums = 6;  // rows, policy loss, entropy, value loss, divergence, clipped rows
 constexpr int kLossBlocks = 2048;
 
-template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>(), team_waves<TEAM>()) void loss_kernel(LossArgs a) {
+template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>(), PER >= 16 || TEAM >= 64 ? 4 : 1) void loss_kernel(LossArgs a) {
   using R = Row<T, TEAM, PER>;
   using raw = typename T::raw;
-  __shared__ double room[TEAM > 64 ? 2 * TEAM / 64 : 1];
-  __shared__ double table[64], sums[kLossSums][team_block<TEAM>() / 64];
+  __shared__ alignas(16) double room[TEAM > 64 ? 4 * TEAM / 64 : 1];
+  __shared__ double table[64], sums[TEAM > 64 ? 1 : kLossSums][4];
   Team<TEAM> team{room};
   fill_powers<TEAM>(table, 1.);
   constexpr int kTeams = team_block<TEAM>() / TEAM;
@@ -1071,7 +1112,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     float x[PER];
     const int rank = team.rank_anew();
     R of(rank, a.n);
-    of.load(logits, mask, x);
+    of.load(logits, mask, from_row(row, a.n_rows, a.logits_stride, a.n), from_row(row, a.n_rows, a.mask_stride, a.n), x);
     const float mine = inside && (!mask || mask[action] != 0) ? T::load(logits[action]) : kNone;
     float top = kNone;
     Oddity odd;
@@ -1100,10 +1141,10 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
         part_end(j, whole, spread);
       }
     }
-    whole = top < __builtin_huge_valf() ? team.sum(whole) : __builtin_nan("");
-    spread = team.sum(spread);
+    team.sum_both(whole, spread);
+    if (!(top < __builtin_huge_valf())) whole = __builtin_nan("");
     const double log_whole = log_of(table, 1., whole);
-    const double entropy = log_whole - 0.69314718055994530942 / 64. * (spread / whole);
+    const double part_of = 1. / whole, entropy = log_whole - 0.69314718055994530942 / 64. * (spread * part_of);
     const double logp = ((double)mine - (double)top) * a.inv_temperature - log_whole;
     double pull = 0.;                     // the policy loss's derivative by the log-probability
     if (use) {
@@ -1132,7 +1173,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     if (a.grad_logits) {
       // scale / temperature * p (entropy_coef (log p + entropy) - pull) for each class; the lane of the one chosen, which has
       // pull added, writes it once more
-      const double by = a.scale * a.inv_temperature, part_of = 1. / whole, bonus = by * a.entropy_coef, h = entropy - log_whole;
+      const double by = a.scale * a.inv_temperature, bonus = by * a.entropy_coef, h = entropy - log_whole;
       const double p = power(table, ((double)mine - (double)top) * a.slope) * part_of;
       const float inv = (float)part_of, least = __builtin_fmaxf((float)(-1000. / a.inv_temperature), -3.4028235e38f);
       const float k3 = (float)(bonus * a.inv_temperature), k4 = (float)(bonus * h - by * pull);
@@ -1156,18 +1197,26 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
       }
     }
   }
+  // (the first lane of each team has the sums of its rows)
   if (!a.partial) return;
+  double* out = a.partial + (size_t)blockIdx.x * kLossSums;
+  if constexpr (TEAM > 64) {
+    if (threadIdx.x == 0) {
 #pragma unroll
-  for (int i = 0; i < kLossSums; ++i) {
-    double v = part[i];
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    if ((threadIdx.x & 63) == 0) sums[i][threadIdx.x >> 6] = v;
-  }
-  __syncthreads();
-  if (threadIdx.x < kLossSums) {
-    double v = 0.;
-    for (int i = 0; i < team_block<TEAM>() / 64; ++i) v += sums[threadIdx.x][i];
-    a.partial[(size_t)blockIdx.x * kLossSums + threadIdx.x] = v;
+      for (int i = 0; i < kLossSums; ++i) out[i] = part[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kLossSums; ++i) {
+      const double v = TEAM == 64 ? part[i] : over_lanes<64>(part[i], [](double a, double b) { return a + b; });
+      if ((threadIdx.x & 63) == 0) sums[i][threadIdx.x >> 6] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < kLossSums) {
+      double v = 0.;
+      for (int i = 0; i < 4; ++i) v += sums[threadIdx.x][i];
+      out[threadIdx.x] = v;
+    }
   }
 }
 
