@@ -105,11 +105,13 @@ template <int LANES, typename V> __device__ __forceinline__ V sum_until(V v) {
     o = moved<0x114>(v);
     v += lane >= 4 ? o : (V)0;
   }
-  if constexpr (LANES == 64) {
+  if constexpr (LANES >= 16) {
     v += moved<0x111>(v);
     v += moved<0x112>(v);
     v += moved<0x114>(v);
     v += moved<0x118>(v);
+  }
+  if constexpr (LANES == 64) {
     const V a = of_lane(v, 15), b = a + of_lane(v, 31), c = b + of_lane(v, 47);
     const int row = (threadIdx.x & 63) >> 4;
     v += row == 0 ? (V)0 : row == 1 ? a : row == 2 ? b : c;
@@ -462,7 +464,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
   }
 }
 
-// ---- few classes: a row in the registers of a lane or of eight
+// ---- few classes: a row in the registers of a lane or of eight or sixteen
 
 // A lane that holds a whole row: each class against every other one.
 template <typename T, int PER> __device__ __forceinline__ Cutoff cut_lane(const float (&x)[PER], const double (&w)[PER], const SampleArgs& a) {
@@ -566,8 +568,8 @@ __device__ __forceinline__ Cutoff cut_by_halves(const float (&x)[PER], const dou
   return cut;
 }
 
-template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(256) void sample_few_kernel(SampleArgs a) {
-  static_assert(TEAM <= 8 && HOW != kSampleBest, "");
+template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(256, PER >= 16 ? 4 : 1) void sample_few_kernel(SampleArgs a) {
+  static_assert(TEAM <= 16 && HOW != kSampleBest, "");
   using R = Row<T, TEAM, PER>;
   constexpr int kTeams = 256 / TEAM;
   __shared__ double table[64];

@@ -172,6 +172,24 @@ def test_many_rows_and_one_mask_for_all(env):
     assert env.pcgrl_sample(torch.empty((0, 5), device=DEV), torch.empty((0,), device=DEV))[0].shape == (0,)
 
 
+@pytest.mark.parametrize("V", [2, 3, 7, 40, 100, 128, 129, 256, 300, 512, 700, 1024, 3000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_draws_do_not_depend_on_how_many_rows_there_are(env, V, dtype):
+    """The kernel is chosen by the number of rows, too: the same rows in a large and in a small batch, one after the other and last."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(V)
+    n = 9001 if V <= 1024 else 600
+    x = (torch.randn((n, V), generator=gen, device=DEV) * 2).to(TYPES[dtype])
+    u = torch.rand((n,), generator=gen, device=DEV)
+    mask = (torch.rand((n, V), generator=gen, device=DEV) < .8).to(torch.uint8)
+    for how in (dict(), dict(top_k=5), dict(top_p=.7, min_p=.01), dict(top_k=max(1, V // 2), top_p=.9), dict(temperature=0.)):
+        a, lp = env.pcgrl_sample(x, u, mask=mask, **how)
+        for at in (slice(0, 3), slice(n - 5, n), slice(100, 101)):
+            b, lp2 = env.pcgrl_sample(x[at], u[at].contiguous(), mask=mask[at], **how)
+            # (the logarithm of the same sum, which is rounded to float32 once)
+            assert torch.equal(a[at], b) and torch.allclose(lp[at], lp2, rtol=2.**-23, atol=1e-9), how
+
+
 def test_rows_beyond_32_bit_offsets(env):
     """Rows so far apart that the last ones lie more than 2^32 bytes and 2^31 elements behind the first."""
     n, V, stride = 70001, 33, 32768
