@@ -992,6 +992,61 @@ __device__ __forceinline__ bool share_by_bins(const Stretch<T, TEAM>& in, const 
   return true;
 }
 
+// For a top_k that the list holds, with the rest of the bin that it ends in: every class that may be kept is listed, ranked once by its
+// logit, for top_k and top_p, and once by its index, for the draw.  False if the list does not hold them, or if top_k keeps all.
+template <typename T, int TEAM>
+__device__ __forceinline__ bool draw_from_list(const Stretch<T, TEAM>& in, const Weigh& weigh, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double least,
+                                               float scale, double whole, int64_t row) {
+  using C = CutRoom<TEAM>;
+  constexpr int kOwn = C::kBins / TEAM, kMost = C::kList < TEAM ? C::kList : TEAM;
+  const int rank = Team<TEAM>::rank();
+  if (rank == 0) m.listed = m.bin = 0;
+  const BinSums<TEAM> sums(team, m, rank, true);
+  if (sums.all <= a.top_k) return false;
+  if (TEAM == 64) team.sync();
+  int seen = sums.seen;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int n = m.count[rank * kOwn + i];
+    if (seen < a.top_k && a.top_k <= seen + n) m.bin = seen + n <= kMost ? rank * kOwn + i : -1;
+    seen += n;
+  }
+  team.sync();
+  const int bin = m.bin;
+  if (bin < 0) return false;
+  in.each([&](float x, int index) {
+    if (x != kNone && C::bin_of(weigh.top - x, scale) <= bin) m.put(class_key<T>(x), index, weigh(x));
+  });
+  team.sync();
+  const int listed = m.listed;
+  typename C::Entry e{0, 0.};
+  double before = 0.;
+  int first = a.top_k;
+  if (rank < listed) {
+    e = m.list[rank];
+    first = 0;
+    m.rank_of(e.order, before, first);
+    if (first == a.top_k - 1) m.mass_until = before + e.weight;
+  }
+  team.sync();
+  const bool keep = first < a.top_k && (!(a.top_p < 1.) || before < a.top_p * m.mass_until) && e.weight >= least;
+  if (rank < listed) m.list[rank].weight = keep ? e.weight : 0.;
+  team.sync();
+  if (keep) {
+    const Cutoff it = C::cutoff(e.order);
+    double until = 0., all = 0.;
+#pragma unroll 8
+    for (int i = 0; i < listed; ++i) {
+      const typename C::Entry o = m.list[i];
+      until += (uint32_t)o.order >= (uint32_t)e.order ? o.weight : 0.;  // (turned round: an index no larger)
+      all += o.weight;
+    }
+    const double target = uniform_of(a, row) * all;
+    if (until > target && until - e.weight <= target) put_draw(a, row, it.index, T::load(in.row[it.index]), weigh.top, whole, weigh.table);
+  }
+  return true;
+}
+
 template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), 4) void sample_many_kernel(SampleArgs a) {
   static_assert(TEAM >= 64 && HOW != kSampleBest, "");
   using S = Stretch<T, TEAM>;
@@ -1050,6 +1105,10 @@ template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block
       bool summed = false;
       if (searched) {
         if (TEAM == 64) team.sync();
+        if (a.top_k > 0 && draw_from_list<T, TEAM>(in, weigh, team, a, m, least, scale, whole, row)) {
+          team.sync();
+          continue;
+        }
         if (a.top_k == 0) {
           summed = share_by_bins<T, TEAM>(in, weigh, team, m, a.top_p * whole, least, scale, mine);
           if (summed) {
