@@ -315,7 +315,7 @@ int pcgrl_unpack_obs(const pcgrl_ctx* ctx, const uint8_t* packed, void* out, int
  * The calls below take a context only for its device; they neither read nor change its environments
  * (pcgrl_step_logits excepted), keep nothing from one call to the next, allocate nothing and may be captured
  * into a HIP graph.  Different calls may run at the same time on different streams.  Element types:
- * PCGRL_UNPACK_F16 / _BF16 / _F32.  Every array is aligned to its element size.
+ * PCGRL_UNPACK_F16 / _BF16 / _F32.  Every array is aligned to its element size.  Numbers of rows and strides are below 2^31.
  *
  * Logits have one row for each decision and one class for each choice: a tile type for the agent's cell
  * (as pcgrl_step takes it), or a cell and a tile type for a policy that chooses both.  A class may
@@ -339,7 +339,8 @@ typedef struct {
  * logit, equal ones by index, a class is kept while it is among the first top_k, while the sum of the
  * weights before it is below top_p times the sum of what top_k left, and while w >= min_p.  The
  * action is the first kept class, by index, at which the running sum of the kept weights exceeds
- * uniform times their sum; weights are rounded to 2^-39 of the largest or finer, and summed exactly.
+ * uniform times their sum; weights are rounded to the nearest multiple of 2^-38 of the largest, and summed
+ * exactly.
  *   logits   : device, [n_rows][logits_stride] elements
  *   mask     : device, uint8 [n_rows][mask_stride], or NULL
  *   uniform  : device, float32 [n_rows] in [0, 1) (what is outside or NaN counts as the nearest such number,

@@ -2,8 +2,9 @@
 // advantages of a rollout.
 //
 // A row of logits belongs to a team of TEAM threads (one lane, a part of a wavefront, a wavefront, a
-// workgroup), which holds all of it in registers, PER classes a thread: one read of HBM, whatever is
-// computed of it.
+// workgroup), which holds all of it in registers, PER classes a thread, or in LDS: one read of HBM, whatever is
+// computed of it.  What an action or the clipping of a ratio depends on is computed in 64 bits, which this part does at the rate
+// of 32; it is what most of these kernels are bound by.
 #pragma once
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -279,12 +280,6 @@ template <typename T, int TEAM, int PER> struct Row {
       pieces = (w + 1) * all / W - from;
       first = (from * 64 + (rank & 63)) * VEC;
     }
-  }
-  // the wavefront of a class: the last one that begins at its piece or before
-  __device__ __forceinline__ int wave_of(int index) const {
-    constexpr int W = TEAM < 64 ? 1 : TEAM / 64;
-    const int all = (n + 64 * VEC - 1) / (64 * VEC), piece = index / (64 * VEC);
-    return ((piece + 1) * W - 1) / all;
   }
   __device__ __forceinline__ bool has(int c) const { return TEAM < 64 || c < pieces; }  // (the same for a wavefront)
   __device__ __forceinline__ int begin(int c) const { return first + c * LANES * VEC; }
@@ -841,20 +836,24 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
   constexpr int kOwn = C::kBins / TEAM;
   const int rank = Team<TEAM>::rank();
   Cutoff cut{0, 0x7fffffff};
-  bool by_mass = a.top_k == 0;
-  float from = weigh.top, to = low, by = scale;  // the logits that are binned, and how
+  bool by_mass = a.top_k == 0, binned = by_mass, whole_row = true;  // (for top_k the numbers are there, but not the weights)
+  // the logits that are binned, and how: the whole row by their distances, part of it by their keys, of which two that differ can
+  // always be told apart
+  float from = weigh.top, to = low;
+  uint64_t by = 0;
   double mass_before = 0.;                       // of the logits above them
   int count_before = 0;
   auto inside = [&](float x) { return x <= from && x >= to && x != kNone; };
+  auto bin_of = [&](float x) { return whole_row ? C::bin_of(from - x, scale) : (int)((uint64_t)(class_key<T>(from) - class_key<T>(x)) * by >> 32); };
 #pragma unroll 1
-  for (bool binned = true;; binned = false) {
+  for (;; binned = false) {
     if (!binned) {
       team.sync();
       m.clear(rank);
       team.sync();
       in.each([&](float x, int) {
         if (inside(x)) {
-          const int b = C::bin_of(from - x, by);
+          const int b = bin_of(x);
           unsafeAtomicAdd(&m.mass[b], weigh(x));
           if (a.top_k > 0) atomicAdd(&m.count[b], 1);
         }
@@ -864,7 +863,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
     const BinSums<TEAM> sums(team, m, rank, a.top_k > 0);
     double run = sums.run + mass_before;
     int seen = sums.seen + count_before;
-    if (!by_mass && binned && sums.all <= a.top_k) by_mass = true;  // top_k keeps all
+    if (!by_mass && whole_row && sums.all <= a.top_k) by_mass = true;  // top_k keeps all
     if (by_mass && !(a.top_p < 1.)) break;
     const double share = a.top_p * whole;
 #pragma unroll
@@ -884,7 +883,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
     team.sync();
     const int bin = m.bin;
     in.each([&](float x, int index) {
-      if (inside(x) && C::bin_of(from - x, by) == bin) m.put(class_key<T>(x), index, weigh(x));
+      if (inside(x) && bin_of(x) == bin) m.put(class_key<T>(x), index, weigh(x));
     });
     team.sync();
     const int listed = m.listed;
@@ -893,7 +892,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
     if (listed > C::kList) {
       float most = kNone, least = -kNone;
       in.each([&](float x, int) {
-        if (inside(x) && C::bin_of(from - x, by) == bin) {
+        if (inside(x) && bin_of(x) == bin) {
           most = __builtin_fmaxf(most, x);
           least = __builtin_fminf(least, x);
         }
@@ -902,7 +901,8 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
       from = most;
       to = least;
       if (to < from) {
-        by = (float)C::kBins / (from - to);
+        by = ((uint64_t)C::kBins << 32) / ((uint64_t)(class_key<T>(from) - class_key<T>(to)) + 1);
+        whole_row = false;
         continue;
       }
       // all equal: the first few by index, as many as it takes
@@ -936,9 +936,9 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
     by_mass = true;  // top_p, of what top_k has left
     from = weigh.top;
     to = low;
-    by = scale;
     mass_before = 0.;
     count_before = 0;
+    whole_row = true;
   }
   return cut;
 }
@@ -1051,7 +1051,7 @@ template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block
   static_assert(TEAM >= 64 && HOW != kSampleBest, "");
   using S = Stretch<T, TEAM>;
   constexpr int kTeams = team_block<TEAM>() / TEAM;
-  extern __shared__ char rows_lds[];
+  extern __shared__ __attribute__((aligned(16))) char rows_lds[];
   __shared__ double table[64], room[TEAM > 64 ? 2 * TEAM / 64 : 1];
   __shared__ CutRoom<TEAM> cut_room[HOW == kSampleCut ? kTeams : 1];
   Team<TEAM> team{room};
@@ -1087,8 +1087,11 @@ template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block
       mine += w;
       if (HOW == kSampleCut && searched) {
         const int b = m.bin_of(top - x, scale);
-        if (w > 0.) unsafeAtomicAdd(&m.mass[b], w);
-        if (a.top_k > 0 && x != kNone) atomicAdd(&m.count[b], 1);
+        if (a.top_k == 0) {
+          if (w > 0.) unsafeAtomicAdd(&m.mass[b], w);
+        } else if (x != kNone) {
+          atomicAdd(&m.count[b], 1);
+        }
       }
     });
     const double whole = team.sum(mine, before, here);

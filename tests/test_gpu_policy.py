@@ -57,13 +57,14 @@ def make_mask(rng, n, V):
     return mask
 
 
-def check_sample(env, logits, mask, u, **how):
+def check_sample(env, logits, mask, u, settled=.6, **how):
+    """Actions of rows whose target is `sure` to be inside its class, which more than `settled` of them have to be."""
     n, V = logits.shape
     actions, logps = env.pcgrl_sample(logits, gpu(u, torch.float32), mask=None if mask is None else gpu(mask), **how)
     want, want_lp, room = policy_oracle.sample(wide64(logits), mask, u, **how)
     actions, logps = actions.cpu().numpy(), wide64(logps)
     sure = room > V * 2.**-39 + 1e-12
-    assert sure.mean() > .6
+    assert sure.mean() > settled
     assert np.array_equal(actions[sure], want[sure])
     lp = want_lp[sure]
     assert np.all(np.abs(logps[sure] - lp) <= np.abs(lp) * HALF[torch.float32] + V * 2.**-39 + 1e-12)
@@ -131,6 +132,27 @@ def test_rows_without_a_choice_and_odd_values(env, V, how):
     flat = -math.log(V) if how.get("temperature") != 0 else 0.
     assert lp[0] == lp[1] == 0 and math.isnan(lp[2]) and math.isnan(lp[3]) and lp[4] == lp[5] == lp[7] == 0
     assert abs(lp[6] - flat) <= 1e-6 * (1 + abs(flat)) and lp[6] == lp[8]
+
+
+@pytest.mark.parametrize("V", [300, 1000, 1024, 2500, 8192, 20000, 32768])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_classes_close_together(env, V, dtype):
+    """Truncations where a great many logits are equal or next to each other, beside few that are far away: values that
+    are one step apart, down to the smallest there are, two values, a few values, zeros of both signs, huge ones."""
+    rng = np.random.default_rng(V)
+    t = TYPES[dtype]
+    step = 2.**-23 if dtype == "f32" else 2.**-7
+    rows = [1 + step * rng.integers(0, 2, V), 1 + step * rng.integers(0, 40, V), step * rng.integers(-3, 3, V), rng.integers(0, 3, V) * 1., np.where(rng.random(V) < .5, 0., -0.),
+            rng.integers(0, 900, V) * 2.**-126, rng.integers(0, 5, V) * 2.**-130, np.where(rng.random(V) < .01, 9., 1 + step * rng.integers(0, 2, V)), 3e38 - 1e37 * rng.integers(0, 3, V),
+            np.where(rng.random(V) < .5, -1e9, 0.), np.where(np.arange(V) == V // 2, 3e38, -3e38), np.full(V, -7.)]
+    x = gpu(np.stack(rows), torch.float64).to(t)
+    # The first numbers times 1000 are whole, so that with equal weights of 20 000 classes each target is a class's border to within the rounding of
+    # the number to 32 bits (2^-25, below the 2^-24.7 that V 2^-39 is): such rows are no test of the action, only the others and the second numbers are.
+    u = (np.arange(len(rows)) * .079 + .03).astype(np.float32)
+    between = ((np.arange(len(rows)) + 1) * .6180339887 % 1).astype(np.float32)
+    for how in (dict(top_k=V // 2), dict(top_k=40), dict(top_p=.6), dict(top_k=V - 1, top_p=.9), dict(top_k=V // 3, top_p=.5, min_p=.9), dict(temperature=1e6, top_p=.3), dict(temperature=1e-6, top_k=200)):
+        check_sample(env, x, None, u, settled=-1, **how)
+        check_sample(env, x, None, between, **how)
 
 
 def test_uniform_numbers_outside_and_zeros_of_both_signs(env):

@@ -26,7 +26,7 @@ def sample(how=None, ctx=CTX, logits=P, mask=None, uniform=P, n_rows=5, actions=
 @pytest.mark.parametrize("rc,more", [
     (NULL, dict(ctx=None)), (NULL, dict(how=False)), (NULL, dict(logits=None)), (NULL, dict(uniform=None)), (NULL, dict(actions=None)),
     (CONFIG, dict(type=0)), (CONFIG, dict(type=4)), (CONFIG, dict(type=-1)), (CONFIG, dict(n_classes=0)), (CONFIG, dict(n_classes=32769, logits_stride=32769)),
-    (CONFIG, dict(n_rows=-1)), (CONFIG, dict(logits_stride=6)), (CONFIG, dict(logits_stride=0)), (CONFIG, dict(logits_stride=-7)),
+    (CONFIG, dict(n_rows=-1)), (CONFIG, dict(n_rows=2**31)), (CONFIG, dict(logits_stride=2**31)), (CONFIG, dict(logits_stride=6)), (CONFIG, dict(logits_stride=0)), (CONFIG, dict(logits_stride=-7)),
     (CONFIG, dict(mask=P, mask_stride=6)), (CONFIG, dict(mask=P, mask_stride=-1)),
     (CONFIG, dict(temperature=-1.0)), (CONFIG, dict(temperature=math.nan)), (CONFIG, dict(temperature=math.inf)), (CONFIG, dict(temperature=1e-31)),
     (CONFIG, dict(top_p=0.0)), (CONFIG, dict(top_p=-0.5)), (CONFIG, dict(top_p=math.nan)), (CONFIG, dict(min_p=-0.1)), (CONFIG, dict(min_p=1.1)),
@@ -63,7 +63,7 @@ def policy_loss(ctx=CTX, null=False, **more):
 @pytest.mark.parametrize("rc,more", [
     (NULL, dict(ctx=None)), (NULL, dict(null=True)), (NULL, dict(logits=None)), (NULL, dict(actions=None)), (NULL, dict(advantages=None)),
     (NULL, dict(values=P)), (NULL, dict(workspace=None)), (CONFIG, dict(type=0)), (CONFIG, dict(type=9)), (CONFIG, dict(n_classes=0)),
-    (CONFIG, dict(n_classes=40000, logits_stride=40000, grad_stride=40000)), (CONFIG, dict(n_rows=-5)), (CONFIG, dict(logits_stride=5)), (CONFIG, dict(grad_stride=6)),
+    (CONFIG, dict(n_classes=40000, logits_stride=40000, grad_stride=40000)), (CONFIG, dict(n_rows=-5)), (CONFIG, dict(n_rows=2**40)), (CONFIG, dict(logits_stride=5)), (CONFIG, dict(grad_stride=6)),
     (CONFIG, dict(mask=P, mask_stride=3)), (CONFIG, dict(temperature=0.0)), (CONFIG, dict(temperature=math.nan)), (CONFIG, dict(temperature=-1.0)),
     (CONFIG, dict(clip_low=-.1)), (CONFIG, dict(clip_low=1.1)), (CONFIG, dict(clip_high=-.1)), (CONFIG, dict(clip_high=math.inf)), (CONFIG, dict(clip_high=math.nan)),
     (CONFIG, dict(entropy_coef=math.nan)), (CONFIG, dict(value_coef=math.inf)), (CONFIG, dict(scale=math.nan)), (CONFIG, dict(logits=P + 2)), (CONFIG, dict(actions=P + 1)),
