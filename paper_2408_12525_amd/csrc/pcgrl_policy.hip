@@ -211,7 +211,7 @@ int pcgrl_advantages(const pcgrl_ctx* ctx, const float* reward, const uint8_t* d
   if (overlap(advantages, out, returns, out)) return PCGRL_E_CONFIG;
   DeviceGuard guard(device_of(ctx));
   if (!guard.ok) return PCGRL_E_DEVICE;
-  AdvantageArgs a{reward, done, values, advantages, returns, n_steps, n_envs, 0, n_steps, discount, discount * trace};
+  AdvantageArgs a{reward, done, values, advantages, returns, n_steps, n_envs, 0, n_steps, discount, discount * trace, discount * trace > 0. ? 1e-300 : 0.};
   const int groups = share_steps(&a);
   const dim3 block(kAdvantageThreads), grid((unsigned)((n_envs + (1 << a.envs_log2) - 1) >> a.envs_log2), (unsigned)groups);
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -1309,7 +1309,7 @@ struct AdvantageArgs {
   int32_t n_steps, n_envs;
   int32_t envs_log2;  // environments of a workgroup
   int32_t group;      // steps of a workgroup: a multiple of what it takes at a time, or all
-  double discount, decay;  // decay: discount * trace
+  double discount, decay, least;  // decay: discount * trace; least: of a product of them
 };
 
 constexpr int kAdvantageThreads = 256, kAdvantageSteps = 8;
@@ -1319,8 +1319,13 @@ constexpr int kAdvantageThreads = 256, kAdvantageSteps = 8;
 constexpr int kAdvantageAll = 0, kAdvantageSum = 1, kAdvantageApply = 2;
 constexpr int kAdvantageEach = 8;  // groups of a thread of the launch in the middle
 
-// (a factor of 0 is the end of an episode: what is behind it does not count, be it infinite or no number)
-__device__ __forceinline__ double after_it(double factor, double term, double behind) { return factor == 0. ? term : __builtin_fma(factor, behind, term); }
+// A stretch of steps makes term + factor * behind of the advantage behind it.  A factor of -1 is the end of an episode in it:
+// what is behind that does not count, be it infinite or no number.  Products stop at `least`, 1e-300, so that what is infinite
+// stays so over however many steps (a finite advantage times that is nothing); with a decay of 0 they are 0.
+__device__ __forceinline__ double after_it(double factor, double term, double behind) { return factor < 0. ? term : __builtin_fma(factor, behind, term); }
+__device__ __forceinline__ double both_factors(double front, double back, double least) {
+  return front < 0. || back < 0. ? -1. : __builtin_fmax(front * back, least);
+}
 
 // Between the launches the factor and the term of group g + 1, and then the advantage behind group g, lie in the
 // first rows of group g's own advantages, which the last launch reads before it writes them.
@@ -1336,8 +1341,8 @@ __device__ __forceinline__ double take(const float* at, int64_t n) {
 // What the threads of a workgroup behind this one make of the advantage behind them all: thread c E + e has steps behind
 // those of thread (c - 1) E + e.  Sets `behind` to the advantage behind this thread's steps and returns that before the
 // workgroup's first; `factor_all`, if asked for, is multiplied by all factors.
-template <bool ALL> __device__ __forceinline__ double join_steps(int envs_log2, double factor, double term, double& behind, double& factor_all, double (*factors)[64],
-                                                        double (*terms)[64]) {
+template <bool ALL> __device__ __forceinline__ double join_steps(int envs_log2, double least, double factor, double term, double& behind, double& factor_all,
+                                                                   double (*factors)[64], double (*terms)[64]) {
   constexpr int kWaves = kAdvantageThreads / 64;
   const int E = 1 << envs_log2, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // within a wavefront: this thread's steps and all behind them
@@ -1346,7 +1351,7 @@ template <bool ALL> __device__ __forceinline__ double join_steps(int envs_log2, 
     const double f2 = __shfl_down(f, d), t2 = __shfl_down(t, d);
     if (lane + d < 64) {
       t = after_it(f, t, t2);
-      f *= f2;
+      f = both_factors(f, f2, least);
     }
   }
   const int per = E < 64 ? 1 : E >> 6;      // wavefronts side by side on the same steps
@@ -1363,7 +1368,7 @@ template <bool ALL> __device__ __forceinline__ double join_steps(int envs_log2, 
     if (per > 1 && (w & (per - 1)) != (wave & (per - 1))) continue;
     if (w == wave) mine = behind;
     behind = after_it(factors[w][col], terms[w][col], behind);
-    if (ALL) factor_all *= factors[w][col];
+    if (ALL) factor_all = both_factors(factors[w][col], factor_all, least);
   }
   // behind this thread's steps are those of the lanes behind it, and then what is behind the wavefront
   const double f2 = E < 64 ? __shfl_down(f, E) : 1., t2 = E < 64 ? __shfl_down(t, E) : 0.;
@@ -1425,16 +1430,16 @@ template <typename T, int MODE> __global__ __launch_bounds__(kAdvantageThreads) 
         value[i] = T::load(v[i]);
         error[i] = (double)r[i] + (end ? 0. : a.discount * (double)T::load(v[i + 1])) - (double)value[i];
         term = end ? error[i] : __builtin_fma(a.decay, term, error[i]);
-        factor = end ? 0. : factor * a.decay;
+        factor = end ? -1. : both_factors(a.decay, factor, a.least);
         ends |= end ? 1u << i : 0u;
       }
     }
     if (top - C * L > lo) fetch(base - C * L);
     if (C > 1) {
-      behind = join_steps<MODE == kAdvantageSum>(a.envs_log2, factor, term, mine, factor_all, factors, terms);
+      behind = join_steps<MODE == kAdvantageSum>(a.envs_log2, a.least, factor, term, mine, factor_all, factors, terms);
     } else {
       behind = after_it(factor, term, behind);
-      factor_all *= factor;
+      factor_all = both_factors(factor, factor_all, a.least);
     }
     if (MODE != kAdvantageSum) {
 #pragma unroll
@@ -1474,10 +1479,10 @@ __global__ __launch_bounds__(kAdvantageThreads) void advantages_join_kernel(Adva
 #pragma unroll
   for (int i = kAdvantageEach - 1; i >= 0; --i) {
     term = after_it(f[i], t[i], term);
-    factor *= f[i];
+    factor = both_factors(f[i], factor, a.least);
   }
   double behind = 0., unused = 1.;
-  join_steps<false>(a.envs_log2, factor, term, behind, unused, factors, terms);
+  join_steps<false>(a.envs_log2, a.least, factor, term, behind, unused, factors, terms);
 #pragma unroll
   for (int i = kAdvantageEach - 1; i >= 0; --i) {
     if (live && i < each && first + i < groups - 1) {

@@ -429,6 +429,27 @@ def test_nothing_passes_the_end_of_an_episode(env, T, n):
     assert bool(torch.isfinite(env.pcgrl_advantages(gpu(reward), gpu(done), gpu(values), .99, .95)[0]).all())
 
 
+@pytest.mark.parametrize("T,n", [(5, 3), (40, 70), (300, 40), (2000, 2), (6000, 3), (33, 5000)])
+@pytest.mark.parametrize("discount,trace", [(.99, .95), (.5, .5), (1., 0.), (0., 1.), (1e-200, 1.)])
+def test_infinite_and_missing_rewards(env, T, n, discount, trace):
+    """NaN and infinity reach every step before them in their episode, however far, and no others: with a trace of 0 too, as
+    0 times infinity is NaN."""
+    rng = np.random.default_rng(T)
+    reward, values = rng.normal(size=(T, n)).astype(np.float32), rng.normal(size=(T + 1, n)).astype(np.float32)
+    done = np.zeros((T, n), np.uint8)
+    done[T // 3, ::2] = 1
+    reward[T - 1, 0], reward[T - 2, 1 % n], values[T, 2 % n] = np.inf, np.nan, -np.inf
+    reward[T // 2, n // 2] = -np.inf
+    adv, ret = env.pcgrl_advantages(gpu(reward), gpu(done), gpu(values), discount, trace)
+    with np.errstate(invalid="ignore"):
+        want, back = policy_oracle.advantages(reward, done, values, discount, trace)
+    for got, exact in ((wide64(adv), want), (wide64(ret), back)):
+        plain = np.isfinite(exact)
+        assert np.array_equal(got[~plain], exact[~plain], equal_nan=True) and (~plain).any()
+        room = 1e-13 * np.abs(exact[plain]).max()
+        assert np.all(np.abs(got[plain] - exact[plain]) <= np.abs(exact[plain]) * HALF[torch.float32] + room)
+
+
 def test_no_steps_and_no_environments(env):
     for T, n in ((0, 4), (4, 0)):
         e = lambda t, steps=T: torch.empty((steps, n), dtype=t, device=DEV)  # noqa: E731
