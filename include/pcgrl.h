@@ -351,14 +351,15 @@ typedef struct {
  *              with mask and temperature, without top_k, top_p and min_p (the policy that
  *              pcgrl_policy_loss differentiates); 0 at temperature 0 and where nothing may be chosen, NaN
  *              where a logit is NaN or +infinity
- * Errors: E_NULL; E_CONFIG if a field of *how or n_rows is out of range or a pointer is misaligned. */
+ * Errors: E_NULL; E_CONFIG if a field of *how or n_rows is out of range, a pointer is misaligned, or an output
+ * overlaps an input or the other output. */
 int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask,
                  const float* uniform, int64_t n_rows, int32_t* actions, float* log_probs, void* stream);
 
 /* pcgrl_sample for every environment, and pcgrl_step with the actions drawn: a step of a policy in the
  * loop as one call (Methods / Training).  n_classes must be the number of tile types, n_rows is the
  * batch; actions is required (and written), log_probs, obs, reward and done may be NULL.
- * Errors: those of both. */
+ * Errors: those of both (what pcgrl_step refuses is refused after the actions have been drawn). */
 int pcgrl_step_logits(pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask,
                       const float* uniform, int32_t* actions, float* log_probs, uint8_t* obs, float* reward,
                       uint8_t* done, void* stream);
@@ -373,9 +374,9 @@ int pcgrl_step_logits(pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* log
  *   reward: device, float32 [n_steps][n_envs]; done: device, uint8 [n_steps][n_envs]
  *   values: device, [n_steps + 1][n_envs] elements of values_type, the last row for the observations
  *           after the last step
- *   advantages: device, float32 [n_steps][n_envs]; returns: the same, or NULL.  Neither may overlap an input.
+ *   advantages: device, float32 [n_steps][n_envs]; returns: the same, or NULL.  Neither may overlap an input or the other.
  * n_steps is 0..2^20, n_envs 0..2^24, discount and trace 0..1.
- * Errors: E_NULL; E_CONFIG if a number is out of range or a pointer is misaligned. */
+ * Errors: E_NULL; E_CONFIG if a number is out of range, a pointer is misaligned, or memory overlaps. */
 int pcgrl_advantages(const pcgrl_ctx* ctx, const float* reward, const uint8_t* done, const void* values,
                      int32_t values_type, int32_t n_steps, int32_t n_envs, double discount, double trace,
                      float* advantages, float* returns, void* stream);
@@ -422,9 +423,10 @@ typedef struct {
  *   d loss / d value     = scale * value_coef * (value - return)
  * Gradients are written, not added: 0 where a class may not be chosen and in rows that are not counted
  * (their advantages, old_log_probs, values and returns are not looked at).  A row counted with a NaN or +infinity
- * among the logits that may be chosen has NaN for gradients.  Elements behind a row's classes are left alone.
- * Probabilities are summed, and ratios compared, in 64 bits; stats are the same from call to call.
- * Errors: E_NULL; E_CONFIG if a field is out of range or a pointer is misaligned. */
+ * among the logits that may be chosen has NaN for the gradients of all its classes.  Elements behind a row's classes
+ * are left alone.  Probabilities are summed, and ratios compared, in 64 bits; stats are the same from call to call.
+ * Errors: E_NULL; E_CONFIG if a field is out of range, a pointer is misaligned, or an output overlaps an input
+ * (other than the two gradients as said above) or another output; padding between rows counts as part of them. */
 int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* loss, void* stream);
 int64_t pcgrl_policy_loss_workspace(void); /* bytes; host side, no GPU work */
 

@@ -26,6 +26,20 @@ bool overlap(const void* p, size_t np, const void* q, size_t nq) {
   const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
   return p && q && a < b + nq && b < a + np;
 }
+struct Memory {
+  const void* at;
+  size_t bytes;
+};
+// Whether any of the outputs shares memory with an input or with another output.
+template <size_t O, size_t I> bool any_overlap(const Memory (&out)[O], const Memory (&in)[I]) {
+  for (size_t o = 0; o < O; ++o) {
+    for (const Memory& i : in)
+      if (overlap(out[o].at, out[o].bytes, i.at, i.bytes)) return true;
+    for (size_t p = 0; p < o; ++p)
+      if (overlap(out[o].at, out[o].bytes, out[p].at, out[p].bytes)) return true;
+  }
+  return false;
+}
 
 int launched() { return hipGetLastError() == hipSuccess ? PCGRL_OK : PCGRL_E_HIP; }
 
@@ -116,6 +130,10 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
   if (misaligned(logits, size) || misaligned(uniform, 4) || misaligned(actions, 4) || misaligned(log_probs, 4)) return PCGRL_E_CONFIG;
   if (bad_rows(n_rows, how->logits_stride, how->n_classes)) return PCGRL_E_CONFIG;
   if (mask && how->mask_stride != 0 && bad_rows(n_rows, how->mask_stride, how->n_classes)) return PCGRL_E_CONFIG;
+  const size_t each = (size_t)n_rows * 4;
+  const Memory in[] = {{logits, span(n_rows, how->logits_stride, how->n_classes, size)}, {mask, span(n_rows, how->mask_stride, how->n_classes, 1)}, {uniform, each}};
+  const Memory out[] = {{actions, each}, {log_probs, each}};
+  if (any_overlap(out, in)) return PCGRL_E_CONFIG;
   DeviceGuard guard(device_of(ctx));
   if (!guard.ok) return PCGRL_E_DEVICE;
   SampleArgs a{};
@@ -205,10 +223,9 @@ int pcgrl_advantages(const pcgrl_ctx* ctx, const float* reward, const uint8_t* d
   if (n_steps == 0 || n_envs == 0) return PCGRL_OK;
   if (!reward || !done || !values || !advantages) return PCGRL_E_NULL;
   if (misaligned(reward, 4) || misaligned(values, size) || misaligned(advantages, 4) || misaligned(returns, 4)) return PCGRL_E_CONFIG;
-  const size_t out = (size_t)n_steps * n_envs * 4, in = (size_t)(n_steps + 1) * n_envs * size;
-  for (const float* o : {advantages, returns})
-    if (overlap(o, out, reward, out) || overlap(o, out, done, out / 4) || overlap(o, out, values, in)) return PCGRL_E_CONFIG;
-  if (overlap(advantages, out, returns, out)) return PCGRL_E_CONFIG;
+  const size_t steps = (size_t)n_steps * n_envs;
+  const Memory in[] = {{reward, steps * 4}, {done, steps}, {values, (steps + n_envs) * size}}, out[] = {{advantages, steps * 4}, {returns, steps * 4}};
+  if (any_overlap(out, in)) return PCGRL_E_CONFIG;
   DeviceGuard guard(device_of(ctx));
   if (!guard.ok) return PCGRL_E_DEVICE;
   AdvantageArgs a{reward, done, values, advantages, returns, n_steps, n_envs, 0, n_steps, discount, discount * trace, discount * trace > 0. ? 1e-300 : 0.};
@@ -248,10 +265,16 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
     if (bad_rows(l->n_rows, l->logits_stride, l->n_classes)) return PCGRL_E_CONFIG;
     if (l->mask && l->mask_stride != 0 && bad_rows(l->n_rows, l->mask_stride, l->n_classes)) return PCGRL_E_CONFIG;
     if (l->grad_logits && bad_rows(l->n_rows, l->grad_stride, l->n_classes)) return PCGRL_E_CONFIG;
-    const bool in_place = l->grad_logits == l->logits && (l->n_rows == 1 || l->grad_stride == l->logits_stride);
-    if (!in_place && overlap(l->grad_logits, span(l->n_rows, l->grad_stride, l->n_classes, size), l->logits,
-                             span(l->n_rows, l->logits_stride, l->n_classes, size)))
-      return PCGRL_E_CONFIG;
+    // (the gradients may lie where what they are of is: nothing else of it is read after them)
+    const int64_t n = l->n_rows;
+    const bool in_place = l->grad_logits == l->logits && (n == 1 || l->grad_stride == l->logits_stride);
+    const size_t row = (size_t)n * 4, value = (size_t)n * size, logits = span(n, l->logits_stride, l->n_classes, size);
+    const Memory in[] = {{in_place ? nullptr : l->logits, logits}, {l->mask, span(n, l->mask_stride, l->n_classes, 1)},
+                         {l->actions, row}, {l->advantages, row}, {l->old_log_probs, row},
+                         {l->grad_values == l->values ? nullptr : l->values, value}, {l->values ? l->returns : nullptr, row}};
+    const Memory out[] = {{l->grad_logits, span(n, l->grad_stride, l->n_classes, size)}, {l->values ? l->grad_values : nullptr, value}, {l->log_probs, row},
+                          {l->entropies, row}, {l->stats, PCGRL_LOSS_STATS * 4}, {l->stats ? l->workspace : nullptr, (size_t)pcgrl_policy_loss_workspace()}};
+    if (any_overlap(out, in)) return PCGRL_E_CONFIG;
   }
   if (l->n_rows == 0 && !l->stats) return PCGRL_OK;
   DeviceGuard guard(device_of(ctx));

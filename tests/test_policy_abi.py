@@ -18,7 +18,7 @@ def sampling(**more):
     return binding.PcgrlSampling(**dict(dict(type=3, n_classes=7, logits_stride=7, mask_stride=7, temperature=1.0, top_p=1.0, min_p=0.0, top_k=0), **more))
 
 
-def sample(how=None, ctx=CTX, logits=P, mask=None, uniform=P, n_rows=5, actions=P, log_probs=P, **more):
+def sample(how=None, ctx=CTX, logits=P, mask=None, uniform=2 * P, n_rows=5, actions=3 * P, log_probs=4 * P, **more):
     how = sampling(**more) if how is None else how
     return binding.load().pcgrl_sample(ctx, C.byref(how) if how else None, logits, mask, uniform, n_rows, actions, log_probs, None)
 
@@ -27,11 +27,13 @@ def sample(how=None, ctx=CTX, logits=P, mask=None, uniform=P, n_rows=5, actions=
     (NULL, dict(ctx=None)), (NULL, dict(how=False)), (NULL, dict(logits=None)), (NULL, dict(uniform=None)), (NULL, dict(actions=None)),
     (CONFIG, dict(type=0)), (CONFIG, dict(type=4)), (CONFIG, dict(type=-1)), (CONFIG, dict(n_classes=0)), (CONFIG, dict(n_classes=32769, logits_stride=32769)),
     (CONFIG, dict(n_rows=-1)), (CONFIG, dict(n_rows=2**31)), (CONFIG, dict(logits_stride=2**31)), (CONFIG, dict(logits_stride=6)), (CONFIG, dict(logits_stride=0)), (CONFIG, dict(logits_stride=-7)),
-    (CONFIG, dict(mask=P, mask_stride=6)), (CONFIG, dict(mask=P, mask_stride=-1)),
+    (CONFIG, dict(mask=5 * P, mask_stride=6)), (CONFIG, dict(mask=5 * P, mask_stride=-1)),
     (CONFIG, dict(temperature=-1.0)), (CONFIG, dict(temperature=math.nan)), (CONFIG, dict(temperature=math.inf)), (CONFIG, dict(temperature=1e-31)),
     (CONFIG, dict(top_p=0.0)), (CONFIG, dict(top_p=-0.5)), (CONFIG, dict(top_p=math.nan)), (CONFIG, dict(min_p=-0.1)), (CONFIG, dict(min_p=1.1)),
-    (CONFIG, dict(min_p=math.nan)), (CONFIG, dict(top_k=-1)), (CONFIG, dict(logits=P + 2)), (CONFIG, dict(logits=ODD, type=1)), (CONFIG, dict(uniform=P + 2)),
-    (CONFIG, dict(actions=P + 2)), (CONFIG, dict(log_probs=P + 1)),
+    (CONFIG, dict(min_p=math.nan)), (CONFIG, dict(top_k=-1)), (CONFIG, dict(logits=P + 2)), (CONFIG, dict(logits=ODD, type=1)), (CONFIG, dict(uniform=2 * P + 2)),
+    (CONFIG, dict(actions=3 * P + 2)), (CONFIG, dict(log_probs=4 * P + 1)),
+    (CONFIG, dict(actions=P)), (CONFIG, dict(actions=P + 136)), (CONFIG, dict(log_probs=P - 16)), (CONFIG, dict(actions=2 * P)), (CONFIG, dict(log_probs=2 * P)),
+    (CONFIG, dict(log_probs=3 * P)), (CONFIG, dict(log_probs=3 * P + 16)), (CONFIG, dict(mask=5 * P, actions=5 * P + 32)), (CONFIG, dict(mask=5 * P, mask_stride=0, log_probs=5 * P + 4)),
     (OK, dict(n_rows=0)), (OK, dict(n_rows=0, logits=None, uniform=None, actions=None, log_probs=None))])
 def test_sample_refuses(rc, more):
     assert sample(**more) == rc
@@ -70,6 +72,9 @@ def policy_loss(ctx=CTX, null=False, **more):
     (CONFIG, dict(advantages=P + 2)), (CONFIG, dict(old_log_probs=P + 2)), (CONFIG, dict(values=P + 2, returns=P)), (CONFIG, dict(values=P, returns=P + 2)),
     (CONFIG, dict(grad_logits=3 * P + 2)), (CONFIG, dict(grad_values=P + 2)), (CONFIG, dict(log_probs=P + 2)), (CONFIG, dict(entropies=P + 1)), (CONFIG, dict(stats=P + 2)),
     (CONFIG, dict(workspace=P + 4)), (CONFIG, dict(grad_logits=P, grad_stride=8)), (CONFIG, dict(grad_logits=P + 28)), (CONFIG, dict(grad_logits=P + 136)),
+    (CONFIG, dict(grad_logits=2 * P)), (CONFIG, dict(log_probs=2 * P)), (CONFIG, dict(log_probs=P + 136)), (CONFIG, dict(entropies=3 * P)), (CONFIG, dict(log_probs=6 * P, entropies=6 * P + 16)),
+    (CONFIG, dict(stats=5 * P)), (CONFIG, dict(workspace=P - 8)), (CONFIG, dict(values=6 * P, returns=7 * P, grad_values=6 * P + 4)), (CONFIG, dict(values=6 * P, returns=7 * P, grad_values=7 * P)),
+    (CONFIG, dict(values=6 * P, returns=7 * P, log_probs=7 * P)), (CONFIG, dict(values=6 * P, returns=7 * P, grad_values=6 * P, entropies=6 * P)), (CONFIG, dict(mask=6 * P, grad_logits=6 * P)),
     (OK, dict(n_rows=0, stats=None, workspace=None, logits=None, grad_logits=None, actions=None, advantages=None))])
 def test_policy_loss_refuses(rc, more):
     assert policy_loss(**more) == rc
