@@ -52,10 +52,21 @@ template <typename F> int by_type(int type, F&& f) {
   if (type == PCGRL_UNPACK_F16) return f(F16{});
   return f(BF16{});
 }
+// (up to 8 classes: a lane that holds exactly as many)
+template <typename F> int by_few_classes(int n, F&& f) {
+  switch (n) {
+    case 1: return f(Shape<1, 1>{});
+    case 2: return f(Shape<1, 2>{});
+    case 3: return f(Shape<1, 3>{});
+    case 4: return f(Shape<1, 4>{});
+    case 5: return f(Shape<1, 5>{});
+    case 6: return f(Shape<1, 6>{});
+    case 7: return f(Shape<1, 7>{});
+    default: return f(Shape<1, 8>{});
+  }
+}
 template <typename F> int by_classes(int n, F&& f) {
-  if (n <= 2) return f(Shape<1, 2>{});
-  if (n <= 4) return f(Shape<1, 4>{});
-  if (n <= 8) return f(Shape<1, 8>{});
+  if (n <= 8) return by_few_classes(n, f);
   if (n <= 64) return f(Shape<8, 8>{});
   if (n <= 128) return f(Shape<8, 16>{});
   if (n <= 256) return f(Shape<16, 16>{});
@@ -172,9 +183,7 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
       using S = decltype(shape);
       return few(shape, cut ? &sample_few_kernel<T, S::kTeam, S::kPer, kSampleCut> : &sample_few_kernel<T, S::kTeam, S::kPer, kSamplePlain>);
     };
-    if (a.n <= 2) return either(Shape<1, 2>{});
-    if (a.n <= 4) return either(Shape<1, 4>{});
-    if (a.n <= 8) return either(Shape<1, 8>{});
+    if (a.n <= 8) return by_few_classes(a.n, either);
     if (a.n <= 64) return either(Shape<8, 8>{});
     // Beyond that, registers for plain draws and where there are enough rows to hide the steps of the halving behind each other, LDS
     // for the rest.  Measured, us for registers / LDS: 4096 rows of 200 classes in bfloat16 3.8 / 7.6, with top_p 13 / 15, with top_k
@@ -318,7 +327,7 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
     if (rc != PCGRL_OK) return rc;
   }
   if (!l->stats) return PCGRL_OK;
-  hipLaunchKernelGGL(loss_sums_kernel, dim3(1), dim3(64 * kLossSums), 0, st, static_cast<const double*>(l->workspace), (int)blocks,
+  hipLaunchKernelGGL(loss_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, static_cast<const double*>(l->workspace), (int)blocks,
                      a.entropy_coef, a.value_coef, a.scale, l->stats);
   return launched();
 }

@@ -240,8 +240,7 @@ template <int TEAM> __device__ __forceinline__ void fill_powers(double* table, d
   if (threadIdx.x < 64) table[threadIdx.x] = unit * 2. * pow2((double)threadIdx.x / 64. - 1.);
   if (TEAM <= 64) __syncthreads();  // (larger teams have a barrier for their largest logit before they read it)
 }
-__device__ __forceinline__ double power(const double* table, double z) {
-  z = __builtin_fmax(z, -64000.);
+__device__ __forceinline__ double power_from(const double* table, double z) {  // (z >= -64000, or NaN)
   const double t = z + 0x1.8p52, r = z - (t - 0x1.8p52);  // the nearest whole number, in the low word of t
   const int n = __double2loint(t);
   double q = 5.732851688640402e-10;                       // (ln(2) / 64)^4 / 4!
@@ -251,6 +250,7 @@ __device__ __forceinline__ double power(const double* table, double z) {
   const double of = table[n & 63];
   return __builtin_ldexp(__builtin_fma(of, q, of), n >> 6);
 }
+__device__ __forceinline__ double power(const double* table, double z) { return power_from(table, __builtin_fmax(z, -64000.)); }
 
 // The natural logarithm of v >= 1 (NaN for infinity and NaN), to about 2^-44, with `table` times 1 / `unit`: what the one in
 // single precision leaves, some 1e-7, by the series.  The library's takes a hundred registers of constants out of a loop.
@@ -264,8 +264,11 @@ __device__ __forceinline__ double log_of(const double* table, double unit, doubl
 // row, in which its lanes' pieces lie side by side, so that running sums go from wavefront to wavefront.  The stretches are as
 // long as the row needs, to one piece, whatever the team could hold.  A piece is read at once, whatever its
 // alignment; the one that the row ends in is read as the last VEC classes, of which those of the piece before are left out.
+// A lane that holds a row holds exactly its classes: what it computes for others in vain is as dear as for these (2 097 152 losses of
+// 7 classes in eight places 43.9 us, in seven 39.0).
 template <typename T, int TEAM, int PER> struct Row {
-  static constexpr int VEC = PER < 16 / (int)sizeof(typename T::raw) ? PER : 16 / (int)sizeof(typename T::raw);
+  static constexpr int VEC = TEAM == 1 || PER < 16 / (int)sizeof(typename T::raw) ? PER : 16 / (int)sizeof(typename T::raw);
+  static constexpr int AT_ONCE = VEC <= 1 ? 1 : VEC <= 2 ? 2 : VEC <= 4 ? 4 : 8;  // classes that a lane with a row reads at once
   static constexpr int PIECES = PER / VEC;
   static constexpr int LANES = TEAM < 64 ? TEAM : 64;
   int first, pieces;  // the thread's first class, and the pieces of its wavefront
@@ -290,70 +293,65 @@ template <typename T, int TEAM, int PER> struct Row {
     return (TEAM > 1 && b > n - VEC ? n - VEC : b) + e;
   }
   // Logits of the classes that may be chosen, kNone for the others.  For a lane that holds a row, `ahead` and `mask_ahead` are the
-  // elements from the row's first to the end of all rows: where there are as many as the lane could hold, it reads so many
+  // elements from the row's first to the end of all rows: where there are as many as AT_ONCE, it reads so many
   // at once, the next row's first ones among them, and not each class by itself.
   __device__ __forceinline__ void load(const typename T::raw* row, const uint8_t* mask, int64_t ahead, int64_t mask_ahead, float (&x)[PER]) const {
+    if constexpr (TEAM == 1) {
+      typename T::raw v[AT_ONCE] = {};
+      uint8_t m[AT_ONCE];
+      if (ahead >= AT_ONCE) {
+        __builtin_memcpy(v, row, sizeof(v));
+      } else {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) v[e] = row[e];
+      }
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] = T::load(v[e]);
+      if (!mask) return;
+      if (mask_ahead >= AT_ONCE) {
+        __builtin_memcpy(m, mask, sizeof(m));
+      } else {  // (the last rows, and one row for all)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) m[e] = mask[e];
+      }
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] = m[e] == 0 ? kNone : x[e];
+      return;
+    }
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) {
-      const int b = begin(c), from = TEAM > 1 && b > n - VEC ? n - VEC : b;
+      const int b = begin(c), from = b > n - VEC ? n - VEC : b;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[c * VEC + e] = kNone;
-      if (TEAM > 1 ? has(c) && b < n : b < n && ahead >= PER) {
+      if (has(c) && b < n) {
         typename T::raw v[VEC];
         __builtin_memcpy(v, row + from, sizeof(v));
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x[c * VEC + e] = T::load(v[e]);
         if (mask) {
           uint8_t m[VEC];
-          if (TEAM > 1 || mask_ahead >= PER) {
-            __builtin_memcpy(m, mask + from, sizeof(m));
-          } else {  // (the last rows, and one row for all)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) m[e] = b + e < n ? mask[b + e] : 0;
-          }
+          __builtin_memcpy(m, mask + from, sizeof(m));
 #pragma unroll
           for (int e = 0; e < VEC; ++e) x[c * VEC + e] = m[e] == 0 ? kNone : x[c * VEC + e];
         }
-        if (TEAM > 1 ? from < b : b + VEC > n) {
+        if (from < b) {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) x[c * VEC + e] = (TEAM > 1 ? from + e < b : b + e >= n) ? kNone : x[c * VEC + e];
-        }
-      } else if (TEAM == 1) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const int i = b + e;
-          if (i < n && (!mask || mask[i] != 0)) x[c * VEC + e] = T::load(row[i]);
+          for (int e = 0; e < VEC; ++e) x[c * VEC + e] = from + e < b ? kNone : x[c * VEC + e];
         }
       }
     }
   }
   __device__ __forceinline__ void store(typename T::raw* row, int c, const float (&g)[VEC]) const {
-    const int b = begin(c), from = TEAM > 1 && b > n - VEC ? n - VEC : b;
+    const int b = begin(c), from = b > n - VEC ? n - VEC : b;
     typename T::raw v[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[e] = T::store(g[e]);
-    if (b + VEC <= n) {
+    if (TEAM == 1 || b + VEC <= n) {
       __builtin_memcpy(row + b, v, sizeof(v));
     } else if (b < n) {
-      if constexpr (TEAM == 1) {  // four, two and one of them
-        constexpr int kSize = sizeof(typename T::raw);
-        const int left = n - b;
-        if (VEC > 4 && left & 4) __builtin_memcpy(row + b, v, 4 * kSize);
-        if (left & 2) {
-          if (VEC > 4 && left & 4) __builtin_memcpy(row + b + 4, v + 4 % VEC, 2 * kSize);
-          else __builtin_memcpy(row + b, v, 2 * kSize);
-        }
-        if (left & 1) {
-          typename T::raw last = v[0];
 #pragma unroll
-          for (int e = 2; e < VEC; e += 2) last = left - 1 == e ? v[e] : last;
-          row[n - 1] = last;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (from + e >= b) row[from + e] = v[e];
-      }
+      for (int e = 0; e < VEC; ++e)
+        if (from + e >= b) row[from + e] = v[e];
     }
   }
 };
@@ -1196,12 +1194,12 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
 #pragma unroll
       for (int i = 0; i < R::VEC; ++i) {
         const int j = c * R::VEC + i;
-        const double y = ((double)x[j] - (double)top) * a.slope, e = power(table, y);
         // (a class that may not be chosen has the weight of 2^-1000, nothing)
+        const double y = __builtin_fmax(((double)x[j] - (double)top) * a.slope, -64000.), e = power_from(table, y);
         w[j] = (float)e;
         done(w[j]);
         whole += e;
-        spread = __builtin_fma(e, __builtin_fmax(y, -64000.), spread);
+        spread = __builtin_fma(e, y, spread);
         part_end(j, whole, spread);
       }
     }
@@ -1284,15 +1282,31 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
   }
 }
 
-// Joins the workgroups' sums, always in the same order.
-__global__ __launch_bounds__(64 * kLossSums) void loss_sums_kernel(const double* partial, int blocks, double entropy_coef, double value_coef,
-                                                                  double scale, float* stats) {
-  __shared__ double sums[kLossSums];
-  const int which = threadIdx.x >> 6;
-  double v = 0.;
-  for (int b = threadIdx.x & 63; b < blocks; b += 64) v += partial[(size_t)b * kLossSums + which];
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  if ((threadIdx.x & 63) == 0) sums[which] = v;
+// Joins the workgroups' sums, always in the same order: thread t has every 768th of them, all of one kind, read at once (a loop
+// that waits for each, a wavefront a kind, took 8 us more for 1280 workgroups).
+constexpr int kSumThreads = 128 * kLossSums, kSumsEach = kLossBlocks * kLossSums / kSumThreads;
+__global__ __launch_bounds__(kSumThreads) void loss_sums_kernel(const double* partial, int blocks, double entropy_coef, double value_coef,
+                                                               double scale, float* stats) {
+  __shared__ double some[kSumThreads], sums[kLossSums];
+  double v[kSumsEach];
+#pragma unroll
+  for (int i = 0; i < kSumsEach; ++i) {
+    const int at = threadIdx.x + i * kSumThreads;
+    v[i] = at < blocks * kLossSums ? partial[at] : 0.;
+  }
+#pragma unroll
+  for (int d = kSumsEach / 2; d > 0; d /= 2) {
+#pragma unroll
+    for (int i = 0; i < d; ++i) v[i] += v[i + d];
+  }
+  some[threadIdx.x] = v[0];
+  __syncthreads();
+  const int which = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (which < kLossSums) {
+    const double both = some[which + kLossSums * lane] + some[which + kLossSums * (lane + 64)];
+    const double sum = over_lanes<64>(both, [](double a, double b) { return a + b; });
+    if (lane == 0) sums[which] = sum;
+  }
   __syncthreads();
   if (threadIdx.x == 0) stats[0] = (float)(scale * (sums[1] - entropy_coef * sums[2] + value_coef * sums[3]));
   if (threadIdx.x < kLossSums) stats[1 + threadIdx.x] = (float)sums[threadIdx.x];
