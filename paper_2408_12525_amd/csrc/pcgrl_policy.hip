@@ -43,7 +43,7 @@ template <size_t O, size_t I> bool any_overlap(const Memory (&out)[O], const Mem
 
 int launched() { return hipGetLastError() == hipSuccess ? PCGRL_OK : PCGRL_E_HIP; }
 
-// Calls f with the type and with the team and the classes a thread of the smallest team that holds a row.
+// By type, and by the team and the classes a thread that hold a row of n classes.
 template <int TEAM, int PER> struct Shape {
   static constexpr int kTeam = TEAM, kPer = PER;
 };
@@ -52,7 +52,9 @@ template <typename F> int by_type(int type, F&& f) {
   if (type == PCGRL_UNPACK_F16) return f(F16{});
   return f(BF16{});
 }
-// (up to 8 classes: a lane that holds exactly as many)
+// (up to 8 classes: a lane that holds exactly as many.  Beyond that as many lanes as have 8 to 32 classes each: what a row costs besides
+// its classes is shared by the rows of a wavefront.  Measured, us for losses: 20 000 rows of 500 in a wavefront / sixteen lanes 38 / 25, 5000 of 2000 in 256
+// threads / a wavefront 33 / 25, 3000 of 4000 in 256 / 128 32 / 28.5.)
 template <typename F> int by_few_classes(int n, F&& f) {
   switch (n) {
     case 1: return f(Shape<1, 1>{});
@@ -79,7 +81,7 @@ template <typename F> int by_classes(int n, F&& f) {
   return f(Shape<1024, 32>{});
 }
 // Workgroups of a loss that the machine holds at once, each of which then takes several rows: four wavefronts a SIMD, five of
-// the smallest teams.  Measured, us for 512 / 1024 / 1280 / 2048 workgroups: 2 097 152 rows of 7 classes 57 / 46 / 45 / 48, 20 000 of
+// the smallest teams.  Measured, us for 512 / 1024 / 1280 / 2048 workgroups: 2 097 152 rows of 7 classes 57 / 46 / 45 / 48 (before other steps), 20 000 of
 // 500 25 / 24 / 26 / 26, 1024 of 16 384 33 / 36 / 36 / 36.
 template <int TEAM> constexpr int64_t resident() {
   constexpr int64_t most = (TEAM <= 8 ? 5 : 4) * (int64_t)65536 / team_block<TEAM>();

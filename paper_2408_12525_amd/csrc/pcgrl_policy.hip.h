@@ -422,7 +422,8 @@ __device__ __forceinline__ double uniform_of(const SampleArgs& a, int64_t row) {
   return u >= 0. ? u < 1. ? u : 1. - 0x1p-24 : 0.;
 }
 
-// The largest logit by itself, for any team.
+// The largest logit by itself, the lowest index of equal ones, for any team: bound by memory (1000 rows of 8000 in bfloat16 4.9 us, 3.3
+// TB/s).
 template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>()) void best_kernel(SampleArgs a) {
   using R = Row<T, TEAM, PER>;
   constexpr int kTeams = team_block<TEAM>() / TEAM;
@@ -561,6 +562,14 @@ __device__ __forceinline__ Cutoff cut_by_halves(const float (&x)[PER], const dou
   return cut;
 }
 
+// Draws of few classes, a row in the registers of one lane, of eight or of sixteen.  With w = 2^((x - top) / (temperature ln 2)), as
+// whole multiples of 2^-38 in doubles, every sum of up to 2^15 of them is exact: the order in which threads add them up does not
+// matter, and an action depends on the numbers given alone.  A row is read once; then come the largest logit, the weights
+// and their sum, the cutoff, what is kept, and the running sum to the target.  One lane holds up to 8 classes: a
+// reduction over lanes is a dozen instructions for each row, and none of these need any; it finds each class's place by
+// comparing all pairs.  Eight or sixteen lanes use DPP moves, and halve the range of keys for the cutoff, 16 or 32 sums.
+// Bound by a launch up to some 20 000 rows (16 384 rows of 7 classes in bfloat16 3.4 us), then by 64-bit instructions: 262 144 rows of
+// 7 4.3 us, 1 000 000 of 4 8.8 us (2.3 TB/s), 100 000 of 64 10.0, 4096 of 200 3.8, with top_p 12.8.
 template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(256, PER >= 16 ? 4 : 1) void sample_few_kernel(SampleArgs a) {
   static_assert(TEAM <= 16 && HOW != kSampleBest, "");
   using R = Row<T, TEAM, PER>;
@@ -1094,6 +1103,14 @@ __device__ __forceinline__ bool draw_from_list(const Stretch<T, TEAM>& in, const
   return true;
 }
 
+// Draws of many classes: the row goes to LDS on its way in, where every pass after that reads it, four classes a thread at a time, and
+// weights are computed again in each rather than kept: registers for 32 doubles a thread would leave a compute unit room for one row, and
+// the phases in which threads wait for each other are what a second row hides.  Without truncations one pass sums the
+// weights, and the draw goes through the wavefront that has it.  For top_p the same pass bins them, a second lists the bin
+// in which the share is reached and sums what is above it.  For a top_k it counts them, and lists what may be kept.
+// Bound by 64-bit instructions, some 35 a class and pass (1024 rows of 28 672 in bfloat16, masked: floor of the bytes 16.3 us, one pass
+// 38, with top_p and its two 90, of which 57 are instructions and 17 atomic additions in LDS), and by waits where rows are few: one row of
+// 16 384 in float32 with top_k 14.3 us, one of 28 672 with top_p 29.
 template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), 4) void sample_many_kernel(SampleArgs a) {
   static_assert(TEAM >= 64 && HOW != kSampleBest, "");
   using S = Stretch<T, TEAM>;
@@ -1210,6 +1227,16 @@ struct LossArgs {
 constexpr int kLossSums = 6;  // rows, policy loss, entropy, value loss, divergence, clipped rows
 constexpr int kLossBlocks = 2048;
 
+// The loss and its gradients, a row in the registers of a team: read once, written once.  With y = (x - top) / temperature,
+// w = e^y and W the sum of w, log p = y - log W and the entropy is log W - (sum of w y) / W: one pass for both sums, in 64 bits.  The second
+// pass needs w, kept in 32 bits, whose rounding is that of the gradient, and log p from x: p (entropy_coef (log p + H) - pull),
+// one fused multiply-add and two products a class.  For the class that was chosen 1 - p loses what p has in 32 bits, so that its
+// gradient is computed in 64 and written over.  Sums of rows go to a workgroup's partials, which a second launch joins, in
+// the same order always (atomics would not, and have to be cleared first); that launch is 4 us of each figure below.
+// Bound by instructions, about 45 a class and 170 a row, which for one lane a row are shared by 64 rows: 2 097 152 rows of
+// 7 in bfloat16 39 us (floor of the bytes 18.6), 300 000 of 50 46, 20 000 of 500 21, 1001 of 8505 in float16 23 (7.9), 1024 of 16 384, masked,
+// 32 (15.5), 500 of 28 672 in float32 36 (21.2).  Rows of a wavefront put together in LDS for full stores were not faster (31 to 32 us for the
+// gradients alone), nor were eight places for 7 classes (43.9).
 template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>(), PER >= 16 || TEAM >= 64 ? 4 : 1) void loss_kernel(LossArgs a) {
   using R = Row<T, TEAM, PER>;
   using raw = typename T::raw;
