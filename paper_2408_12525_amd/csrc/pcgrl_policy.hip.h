@@ -1108,8 +1108,8 @@ __device__ __forceinline__ bool draw_from_list(const Stretch<T, TEAM>& in, const
 // the phases in which threads wait for each other are what a second row hides.  Without truncations one pass sums the
 // weights, and the draw goes through the wavefront that has it.  For top_p the same pass bins them, a second lists the bin
 // in which the share is reached and sums what is above it.  For a top_k it counts them, and lists what may be kept.
-// Bound by 64-bit instructions, some 35 a class and pass (1024 rows of 28 672 in bfloat16, masked: floor of the bytes 16.3 us, one pass
-// 38, with top_p and its two 90, of which 57 are instructions and 17 atomic additions in LDS), and by waits where rows are few: one row of
+// Bound by 64-bit instructions, 34 a class in one pass and 87 in the two for top_p (1024 rows of 28 672 in bfloat16, masked: floor of the bytes
+// 16.3 us, one pass 38, of which 26 are instructions, with top_p 90, of which 65 are), and by waits where rows are few: one row of
 // 16 384 in float32 with top_k 14.3 us, one of 28 672 with top_p 29.
 template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), 4) void sample_many_kernel(SampleArgs a) {
   static_assert(TEAM >= 64 && HOW != kSampleBest, "");
@@ -1233,7 +1233,7 @@ constexpr int kLossBlocks = 2048;
 // one fused multiply-add and two products a class.  For the class that was chosen 1 - p loses what p has in 32 bits, so that its
 // gradient is computed in 64 and written over.  Sums of rows go to a workgroup's partials, which a second launch joins, in
 // the same order always (atomics would not, and have to be cleared first); that launch is 4 us of each figure below.
-// Bound by instructions, about 45 a class and 170 a row, which for one lane a row are shared by 64 rows: 2 097 152 rows of
+// Bound by instructions, about 45 a class and 110 a row, which for one lane a row are shared by 64 rows: 2 097 152 rows of
 // 7 in bfloat16 39 us (floor of the bytes 18.6), 300 000 of 50 46, 20 000 of 500 21, 1001 of 8505 in float16 23 (7.9), 1024 of 16 384, masked,
 // 32 (15.5), 500 of 28 672 in float32 36 (21.2).  Rows of a wavefront put together in LDS for full stores were not faster (31 to 32 us for the
 // gradients alone), nor were eight places for 7 classes (43.9).
