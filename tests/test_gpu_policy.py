@@ -155,6 +155,25 @@ def test_many_classes_close_together(env, V, dtype):
         check_sample(env, x, None, between, **how)
 
 
+@pytest.mark.parametrize("V,n", [(200, 5000), (500, 3000), (1024, 900), (4100, 400), (8192, 400), (8193, 400), (15400, 400), (16384, 400), (30000, 400), (31000, 400),
+                                 (600, 2**22 + 7), (1030, 2**20 + 5), (4100, 2**20 + 300)])
+def test_a_row_is_drawn_alike_whatever_is_drawn_with_it(env, V, n):
+    """However many rows there are, which decides on the threads that a row gets, and also where workgroups take several in turn."""
+    g = torch.Generator(DEV).manual_seed(V)
+    for dtype in TYPES.values() if n < 10000 else [torch.bfloat16]:
+        x = torch.empty((n, V), dtype=dtype, device=DEV).normal_(0, 2, generator=g)
+        u = torch.rand((n,), generator=g, device=DEV)
+        for how in ({}, dict(top_p=.8), dict(top_k=30, top_p=.9), dict(top_k=V // 2, min_p=.01)):
+            actions, logps = env.pcgrl_sample(x, u, **how)
+            for rows in (slice(0, 5), slice(n // 2, n // 2 + 3), slice(n - 4, n)):
+                few, their = env.pcgrl_sample(x[rows], u[rows], **how)
+                assert torch.equal(actions[rows], few) and torch.equal(logps[rows], their)
+            few = actions[-4:].cpu().numpy()
+            want, _, room = policy_oracle.sample(wide64(x[-4:]), None, u[-4:].cpu().numpy(), **how)
+            sure = room > V * 2.**-39 + 1e-12
+            assert np.array_equal(few[sure], want[sure])
+
+
 def test_uniform_numbers_outside_and_zeros_of_both_signs(env):
     x = torch.zeros((6, 4), device=DEV)
     u = torch.tensor([-1., 1., 2., math.nan, math.inf, -math.inf], device=DEV)
