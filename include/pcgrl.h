@@ -397,7 +397,8 @@ typedef struct {
   double temperature;          /* 1e-30 .. 3e38 */
   double clip_low, clip_high;  /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; 0..1 and >= 0 */
   double entropy_coef, value_coef;
-  double scale;                /* of the loss and its gradients, e.g. 1 / rows (more for float16) */
+  double scale;                /* of the loss and its gradients, e.g. 1 / rows (more for float16); scale / temperature, that times
+                                  entropy_coef, and scale * value_coef are at most 1e300 */
   void* grad_logits;           /* [n_rows][grad_stride], or NULL; may be `logits` itself, with its stride */
   int64_t grad_stride;         /* elements, >= n_classes (any for one row) */
   void* grad_values;           /* [n_rows], or NULL; may be `values` itself */
@@ -424,7 +425,9 @@ typedef struct {
  * Gradients are written, not added: 0 where a class may not be chosen and in rows that are not counted
  * (their advantages, old_log_probs, values and returns are not looked at).  A row counted with a NaN or +infinity
  * among the logits that may be chosen has NaN for the gradients of all its classes.  Elements behind a row's classes
- * are left alone.  Probabilities are summed, and ratios compared, in 64 bits; stats are the same from call to call.
+ * are left alone.  Probabilities are summed, and ratios compared, in 64 bits; the gradients of classes other than the action's are
+ * computed from probabilities in 32 bits (below 2^-126 with fewer, below 2^-149 none), and in 64 where a row's factors are not
+ * ordinary ones: from 2^40 up, infinite or no number, or at temperatures beyond 2^-40 .. 2^40.  stats are the same from call to call.
  * Errors: E_NULL; E_CONFIG if a field is out of range, a pointer is misaligned, or an output overlaps an input
  * (other than the two gradients as said above) or another output; padding between rows counts as part of them. */
 int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* loss, void* stream);

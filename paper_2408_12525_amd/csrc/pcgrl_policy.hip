@@ -265,6 +265,10 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
   if (!(l->temperature >= 1e-30 && l->temperature <= 3e38) || !(l->clip_low >= 0. && l->clip_low <= 1.) || !(l->clip_high >= 0.) ||
       !std::isfinite(l->clip_high) || !std::isfinite(l->entropy_coef) || !std::isfinite(l->value_coef) || !std::isfinite(l->scale))
     return PCGRL_E_CONFIG;
+  // (what gradients are multiplied by, with room for a sum of products in 64 bits)
+  constexpr double kMostFactor = 1e300;
+  const double by = l->scale / l->temperature;
+  if (!(std::fabs(by) <= kMostFactor && std::fabs(by * l->entropy_coef) <= kMostFactor && std::fabs(l->scale * l->value_coef) <= kMostFactor)) return PCGRL_E_CONFIG;
   if (l->stats && !l->workspace) return PCGRL_E_NULL;
   if (misaligned(l->stats, 4) || misaligned(l->workspace, 8)) return PCGRL_E_CONFIG;
   if (l->n_rows > 0) {
@@ -312,9 +316,15 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
   a.slope = 64. * 1.44269504088896340736 * a.inv_temperature;
   a.low = 1. - l->clip_low;
   a.high = 1. + l->clip_high;
-  a.entropy_coef = l->entropy_coef;
-  a.value_coef = l->value_coef;
-  a.scale = l->scale;
+  a.by = l->scale * a.inv_temperature;
+  a.bonus = a.by * l->entropy_coef;
+  a.value_by = l->value_coef * l->scale;
+  // (gradients in 32 bits: if all factors are in reach, and that of the logits' distances keeps all its bits)
+  const double bonus = std::fabs(a.bonus);
+  const bool narrow = l->temperature >= 1. / kWidest && l->temperature <= kWidest && bonus < kWidest && (bonus == 0. || bonus / l->temperature > 0x1p-100);
+  a.widest = narrow ? kWidest : -1.;
+  a.bonus_off = narrow ? (float)(a.bonus * a.inv_temperature) : 0.f;
+  a.least = narrow ? (float)(-1000. / a.inv_temperature) : 0.f;
   hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned blocks = 0;
   if (l->n_rows > 0) {
@@ -330,7 +340,7 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
   }
   if (!l->stats) return PCGRL_OK;
   hipLaunchKernelGGL(loss_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, static_cast<const double*>(l->workspace), (int)blocks,
-                     a.entropy_coef, a.value_coef, a.scale, l->stats);
+                     l->entropy_coef, l->value_coef, l->scale, l->stats);
   return launched();
 }
 

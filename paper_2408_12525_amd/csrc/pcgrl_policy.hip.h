@@ -1220,18 +1220,25 @@ struct LossArgs {
   double* partial;      // kLossSums doubles of each workgroup, or NULL
   int64_t n_rows, logits_stride, mask_stride, grad_stride;
   int32_t n;
+  double widest;        // rows whose factors are not below it have their gradients in 64 bits: kWidest, or -1, all
   double slope, inv_temperature, low, high;  // the ratio is clipped to [low, high]
-  double entropy_coef, value_coef, scale;
+  double by, bonus, value_by;  // scale / temperature, that times the entropy's coefficient; scale times the value's
+  float bonus_off, least;      // bonus / temperature; -1000 temperatures
 };
 
 constexpr int kLossSums = 6;  // rows, policy loss, entropy, value loss, divergence, clipped rows
 constexpr int kLossBlocks = 2048;
+// The classes' gradients are computed in 32 bits where what they are multiplied by is below this: then a probability may lose what 32
+// bits do not hold of it, 2^-150, and the gradient is off by no more than 2^-110.
+constexpr double kWidest = 0x1p40;
 
 // The loss and its gradients, a row in the registers of a team: read once, written once.  With y = (x - top) / temperature,
 // w = e^y and W the sum of w, log p = y - log W and the entropy is log W - (sum of w y) / W: one pass for both sums, in 64 bits.  The second
 // pass needs w, kept in 32 bits, whose rounding is that of the gradient, and log p from x: p (entropy_coef (log p + H) - pull),
 // one fused multiply-add and two products a class.  For the class that was chosen 1 - p loses what p has in 32 bits, so that its
-// gradient is computed in 64 and written over.  Sums of rows go to a workgroup's partials, which a second launch joins, in
+// gradient is computed in 64 and written over.  Rows whose factors 32 bits do not hold (very low and very high temperatures, large coefficients,
+// ratios beyond e^28 with an advantage below 0, advantages and ratios that are infinite or no number) have all of theirs
+// computed in 64 bits, from the logits again.  Sums of rows go to a workgroup's partials, which a second launch joins, in
 // the same order always (atomics would not, and have to be cleared first); that launch is 4 us of each figure below.
 // Bound by instructions, about 45 a class and 110 a row, which for one lane a row are shared by 64 rows: 2 097 152 rows of
 // 7 in bfloat16 39 us (floor of the bytes 18.6), 300 000 of 50 46, 20 000 of 500 21, 1001 of 8505 in float16 23 (7.9), 1024 of 16 384, masked,
@@ -1307,7 +1314,7 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
       if (a.values) {
         const double off = use ? (double)T::load(static_cast<const raw*>(a.values)[row]) - (double)a.returns[row] : 0.;
         part[3] += .5 * off * off;
-        if (a.grad_values) static_cast<raw*>(a.grad_values)[row] = T::store((float)(a.value_coef * a.scale * off));
+        if (a.grad_values) static_cast<raw*>(a.grad_values)[row] = T::store((float)(a.value_by * off));
       }
       if (a.log_probs) a.log_probs[row] = use ? (float)logp : 0.f;
       if (a.entropies) a.entropies[row] = use ? (float)entropy : 0.f;
@@ -1315,27 +1322,44 @@ template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block
     if (a.grad_logits) {
       // scale / temperature * p (entropy_coef (log p + entropy) - pull) for each class; the lane of the one chosen, which has
       // pull added, writes it once more
-      const double by = a.scale * a.inv_temperature, bonus = by * a.entropy_coef, h = entropy - log_whole;
+      const double push = a.bonus * (entropy - log_whole) - a.by * pull;
       const double p = power(table, ((double)mine - (double)top) * a.slope) * part_of;
-      const float inv = (float)part_of, least = __builtin_fmaxf((float)(-1000. / a.inv_temperature), -3.4028235e38f);
-      const float k3 = (float)(bonus * a.inv_temperature), k4 = (float)(bonus * h - by * pull);
-      const float chosen = (float)(bonus * p * (logp + entropy) + by * pull * (1. - p));
+      const float chosen = (float)(a.bonus * p * (logp + entropy) + a.by * pull * (1. - p));
       raw* grad = static_cast<raw*>(a.grad_logits) + row * a.grad_stride;
-      forget_classes<TEAM, PER>(x, of.first);
-#pragma unroll
-      for (int c = 0; c < R::PIECES; ++c) {
-        if (!of.has(c)) continue;
-        float g[R::VEC];
-#pragma unroll
-        for (int e = 0; e < R::VEC; ++e) {
-          const int j = c * R::VEC + e;
-          // (of a class that may not be chosen w is 0, and the rest has to be a number)
-          g[e] = w[j] * inv * __builtin_fmaf(k3, __builtin_fmaxf(x[j] - top, least), k4);
-          if (!use) g[e] = 0.f;
+      if (__builtin_expect(use && !(__builtin_fabs(push) < a.widest), 0)) {
+        // (one class after the other, each read once more, so that nothing of this takes registers from the other rows)
+        int64_t again = row;
+        asm volatile("" : "+v"(again));
+        const raw* from = static_cast<const raw*>(a.logits) + again * a.logits_stride;
+        const uint8_t* may = a.mask ? a.mask + again * a.mask_stride : nullptr;
+#pragma unroll 1
+        for (int k = 0; k < of.pieces * R::VEC; ++k) {
+          const int j = of.begin(k / R::VEC) + k % R::VEC;
+          if (j >= a.n) continue;
+          const double off = (double)(may && may[j] == 0 ? kNone : T::load(from[j])) - (double)top, z = off * a.slope;
+          const double e = z < -64000. ? 0. : power_from(table, z);
+          // (what has no probability has no gradient, whatever it would be times; in a row with a NaN that is one)
+          const double g = e > 0. ? e * part_of * (a.bonus * (off * a.inv_temperature) + push) : e * part_of;
+          grad[j] = T::store(j == action ? chosen : (float)g);
         }
-        of.store(grad, c, g);
-        if (use && of.owns(c, action)) grad[action] = T::store(chosen);
-        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        const float inv = (float)part_of, k4 = (float)push;
+        forget_classes<TEAM, PER>(x, of.first);
+#pragma unroll
+        for (int c = 0; c < R::PIECES; ++c) {
+          if (!of.has(c)) continue;
+          float g[R::VEC];
+#pragma unroll
+          for (int e = 0; e < R::VEC; ++e) {
+            const int j = c * R::VEC + e;
+            // (of a class that may not be chosen w is 0, and the rest is a number)
+            g[e] = w[j] * inv * __builtin_fmaf(a.bonus_off, __builtin_fmaxf(x[j] - top, a.least), k4);
+            if (!use) g[e] = 0.f;
+          }
+          of.store(grad, c, g);
+          if (use && of.owns(c, action)) grad[action] = T::store(chosen);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
   }
