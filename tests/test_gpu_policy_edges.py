@@ -14,6 +14,7 @@ import numpy as np
 import pytest
 import torch
 
+import policy_oracle
 from paper_2408_12525_amd import binding, workloads as wl
 
 pytestmark = pytest.mark.gpu
@@ -159,3 +160,152 @@ def test_masked_classes_have_no_gradient_whatever_the_row_is_weighed_by(env, V, 
     got = env.pcgrl_policy_loss(x, gpu(a, torch.int32), gpu(adv), mask=gpu(mask), scale=1.)["grad_logits"]
     assert not bool((got[gpu(mask) == 0] != 0).any())
     check_gradient(got, *gradients(wide64(x), mask, a, adv), t)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [3, 7, 60, 300, 1000, 3000, 9000, 20000])
+def test_actions_drawn_at_any_temperature(env, V, dtype):
+    """From 1e-30 to 3e38, with logits of a policy and of the temperature's size.  Weights are rounded to 2^-39 of the largest or
+    less, so that an action is settled where its target is further from a border than that many of them."""
+    rng, t, n = np.random.default_rng(V), TYPES[dtype], 7 if V < 5000 else 3
+    for T in (1e-30, 1e-22, 1e-10, 1e10, 1e25, 3e38):
+        for spread in (1.5, T / 4):
+            if not 1e-3 < spread < 1e3 and t == torch.float16:
+                continue
+            x = gpu(np.clip(rng.normal(size=(n, V)) * spread, -3.3e38, 3.3e38), torch.float64).to(t)
+            u = rng.random(n).astype(np.float32)
+            for how in (dict(), dict(top_p=.7), dict(top_k=20, top_p=.9), dict(top_k=max(1, V // 2)), dict(min_p=.3, top_p=.8)):
+                a, lp = env.pcgrl_sample(x, gpu(u), temperature=T, **how)
+                want, want_lp, room = policy_oracle.sample(wide64(x), None, u, temperature=T, **how)
+                sure = room > V * 2.**-39 + 1e-12
+                assert sure.any() and np.array_equal(a.cpu().numpy()[sure], want[sure]), (T, spread, how)
+                w = want_lp[sure]
+                with np.errstate(over="ignore"):
+                    near = np.abs(wide64(lp)[sure] - w) <= np.abs(w) * HALF[torch.float32] + V * 2.**-39 + 1e-12
+                assert np.all(near), (T, spread, how)
+
+
+@pytest.mark.parametrize("V,n,dtype", [(2, 700000, "f32"), (7, 700001, "bf16"), (8, 300003, "f16"), (40, 100001, "bf16"), (120, 60000, "f32"), (200, 30001, "f16"), (500, 20003, "bf16"), (600, 9001, "f32"),
+                                       (1500, 9002, "bf16"), (4000, 4500, "f16"), (6000, 2100, "bf16"), (16384, 1100, "bf16"), (16384, 1100, "f32"), (20000, 600, "f32"), (28672, 600, "bf16")])
+def test_losses_of_more_rows_than_the_machine_holds_at_once(env, V, n, dtype):
+    """Workgroups take several rows in turn, rows that do not count among them: every gradient, and the sums over all
+    rows, against the formula in 64 bits, once with and once without old log-probabilities."""
+    t, g = TYPES[dtype], torch.Generator(DEV).manual_seed(V)
+    x = torch.randn((n, V), generator=g, device=DEV).mul_(1.5).to(t)
+    mask = (torch.rand((n, V), generator=g, device=DEV) < .8).to(torch.uint8)
+    a = torch.randint(0, V, (n,), generator=g, device=DEV)
+    counts = torch.rand((n,), generator=g, device=DEV) < .9
+    mask.scatter_(1, a[:, None], counts[:, None].to(torch.uint8))
+    adv, wobble = (torch.randn((n,), generator=g, device=DEV) for _ in range(2))
+    values, returns = torch.randn((n,), generator=g, device=DEV).to(t), torch.randn((n,), generator=g, device=DEV)
+    coef, vcoef, scale, step = .03, .6, 3. / n, max(1, 4_000_000 // V)
+
+    def parts(lo, hi):
+        may = mask[lo:hi] != 0
+        y = x[lo:hi].double().masked_fill(~may, -math.inf)
+        some = may.any(1, keepdim=True)
+        y = torch.where(some, y - y.amax(1, keepdim=True), torch.zeros_like(y))
+        e = torch.where(may, y.exp(), 0.)
+        whole = e.sum(1, keepdim=True).clamp(min=1e-300)
+        return e / whole, torch.where(may, y - whole.log(), 0.)
+
+    own = torch.cat([parts(lo, lo + step)[1].gather(1, a[lo:lo + step, None])[:, 0] for lo in range(0, n, step)])
+    for old in (None, (own + .3 * wobble.double()).float()):
+        lp, h = torch.full((n,), 7., device=DEV), torch.full((n,), 7., device=DEV)
+        got = env.pcgrl_policy_loss(x, a.int(), adv, old_log_probs=old, mask=mask, values=values, returns=returns, entropy_coef=coef, value_coef=vcoef, scale=scale, log_probs=lp, entropies=h)
+        ratio = torch.ones_like(own) if old is None else (own - old.double()).exp()
+        up = adv.double()
+        held = torch.zeros_like(counts) if old is None else ((up > 0) & (ratio > 1.2)) | ((up < 0) & (ratio < .8))
+        near = counts & ((ratio - 1.2).abs().minimum((ratio - .8).abs()) < 1e-9)
+        assert not bool(near.any())
+        u = torch.where(held, 0., -up * ratio)
+        policy = -up * own if old is None else torch.where(held, -up * torch.where(up > 0, 1.2 * torch.ones_like(up), .8 * torch.ones_like(up)), -up * ratio)
+        entropy = torch.zeros_like(own)
+        for lo in range(0, n, step):
+            p, logs = parts(lo, lo + step)
+            rows = slice(lo, lo + len(p))
+            H = -(p * logs).sum(1)
+            entropy[rows] = H
+            chosen = torch.zeros_like(p).scatter_(1, a[rows, None], 1.)
+            inside = mask[rows] != 0
+            want = scale * (u[rows, None] * (chosen - p) + coef * p * (logs + H[:, None]))
+            want = torch.where(counts[rows, None] & inside, want, 0.)
+            size = scale * (u[rows, None].abs() * (chosen + p) + coef * (p + 2.**-128) * (1 + logs.abs() + H[:, None]) + u[rows, None].abs() * 2.**-128)
+            far = (got["grad_logits"][rows].double() - want).abs() - (want.abs() * HALF[t] + size * 8 * 2.**-24 * (1 + HALF[t]) + TINY[t] / 2)
+            assert float(far.max()) <= 0
+            assert not bool((got["grad_logits"][rows][~inside | ~counts[rows, None]] != 0).any())
+        off = values.double() - returns.double()
+        want = torch.where(counts, scale * vcoef * off, 0.)
+        assert bool(((got["grad_values"].double() - want).abs() <= want.abs() * HALF[t] * 1.01 + TINY[t] / 2).all())
+        for out, of in ((lp, own), (h, entropy)):
+            of = torch.where(counts, of, 0.)
+            assert bool(((out.double() - of).abs() <= of.abs() * HALF[torch.float32] + 1e-11).all())
+        terms = [torch.where(counts, v, 0.) for v in (torch.ones_like(own), policy, entropy, .5 * off * off, ratio - 1 - ratio.log(), held.double())]
+        sums, sizes = [float(v.sum()) for v in terms], [float(v.abs().sum()) for v in terms]
+        sizes[4] += float(torch.where(counts, ratio + 1 + ratio.log().abs(), 0.).sum())
+        sums.insert(0, scale * (sums[1] - coef * sums[2] + vcoef * sums[3]))
+        sizes.insert(0, scale * (sizes[1] + coef * sizes[2] + vcoef * sizes[3]))
+        for k, (s, is_of, size) in enumerate(zip(got["stats"].double().tolist(), sums, sizes)):
+            assert abs(s - is_of) <= abs(is_of) * HALF[torch.float32] + size * 1e-12, k
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("V", CLASSES)
+def test_a_nan_or_infinity_shows_in_all_classes_of_its_row(env, V, masked):
+    """Those that may not be chosen among them, and in no other row."""
+    rng = np.random.default_rng(V)
+    for odd in (math.nan, math.inf):
+        x = gpu(rng.normal(size=(6, V)), torch.float32)
+        a = rng.integers(0, V, 6)
+        mask = some_mask(rng, 6, V, a) if masked else None
+        if masked:
+            mask[2, V - 1] = 1
+        x[2, V - 1] = odd
+        x[4, V // 2], a[4] = odd, -1                    # (a row that does not count)
+        adv = rng.normal(size=6).astype(np.float32)
+        for old in (None, gpu(np.full(6, -1.), torch.float32)):
+            got = env.pcgrl_policy_loss(x, gpu(a, torch.int32), gpu(adv), old_log_probs=old, mask=None if mask is None else gpu(mask))
+            bad = torch.isnan(got["grad_logits"])
+            assert bool(bad[2].all()) and not bool(bad[[0, 1, 3, 4, 5]].any()) and not bool(got["grad_logits"][4].any()) and math.isnan(float(got["stats"][0]))
+
+
+@pytest.mark.parametrize("V,n", [(4, 30), (40, 30), (100, 30), (200, 9000), (400, 30), (700, 30), (3000, 30), (9000, 400), (20000, 30), (20000, 400)])
+def test_outputs_left_out(env, V, n):
+    """What a caller of the C interface does not ask for is not written, and changes nothing of the rest."""
+    rng, L, P = np.random.default_rng(V), binding.load(), lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    C = binding.C
+    st = torch.cuda.current_stream(DEV).cuda_stream
+    x, u = gpu(rng.normal(size=(n, V)), torch.bfloat16), gpu(rng.random(n), torch.float32)
+    for how in (dict(), dict(top_p=.8), dict(top_k=30, min_p=.01), dict(top_k=V // 2, top_p=.9), dict(temperature=0.)):
+        want, lp = env.pcgrl_sample(x, u, **how)
+        c = binding.PcgrlSampling(**dict(dict(type=2, n_classes=V, logits_stride=V, mask_stride=V, temperature=1., top_p=1., min_p=0., top_k=0), **how))
+        got = torch.full((n,), 99, dtype=torch.int32, device=DEV)
+        assert L.pcgrl_sample(env.h, C.byref(c), P(x), None, P(u), n, P(got), None, st) == 0
+        assert torch.equal(got, want)
+    act, adv, old = want, gpu(rng.normal(size=n), torch.float32), gpu(np.full(n, -math.log(V)), torch.float32)
+    values, returns = gpu(rng.normal(size=n), torch.bfloat16), gpu(rng.normal(size=n), torch.float32)
+    full = dict(log_probs=torch.empty(n, device=DEV), entropies=torch.empty(n, device=DEV))
+    full.update(env.pcgrl_policy_loss(x, act, adv, old_log_probs=old, values=values, returns=returns, scale=1., **full))
+    room = torch.empty((L.pcgrl_policy_loss_workspace(),), dtype=torch.uint8, device=DEV)
+    for names in ([], ["stats"], ["grad_logits"], ["grad_values"], ["log_probs"], ["entropies"], ["grad_logits", "grad_values"], ["stats", "grad_logits"], ["stats", "grad_values", "entropies"]):
+        outs = {k: torch.full_like(full[k], 5.) for k in names}
+        c = binding.PcgrlLoss(type=2, n_classes=V, n_rows=n, logits=P(x), logits_stride=V, actions=P(act), advantages=P(adv), old_log_probs=P(old), values=P(values), returns=P(returns),
+                              temperature=1., clip_low=.2, clip_high=.2, entropy_coef=.01, value_coef=.5, scale=1., grad_stride=V, workspace=P(room) if "stats" in names else None,
+                              **{k: P(t) for k, t in outs.items()})
+        assert L.pcgrl_policy_loss(env.h, C.byref(c), st) == 0
+        assert all(torch.equal(outs[k], full[k]) for k in names), names
+    # no rows: the statistics alone
+    stats = torch.full((binding.LOSS_STATS,), 5., device=DEV)
+    c = binding.PcgrlLoss(type=2, n_classes=V, n_rows=0, temperature=1., scale=1., stats=P(stats), workspace=P(room))
+    assert L.pcgrl_policy_loss(env.h, C.byref(c), st) == 0 and not bool(stats.any())
+
+
+@pytest.mark.parametrize("T,n", [(1, 5), (50, 70), (300, 5000), (9000, 3), (3000, 600)])
+def test_advantages_without_returns(env, T, n):
+    rng, L = np.random.default_rng(T), binding.load()
+    reward, done = gpu(rng.normal(size=(T, n)), torch.float32), gpu(rng.random((T, n)) < .02).to(torch.uint8)
+    values = gpu(rng.normal(size=(T + 1, n)), torch.float32)
+    want, _ = env.pcgrl_advantages(reward, done, values, .99, .95)
+    got = torch.full((T, n), 5., device=DEV)
+    assert L.pcgrl_advantages(env.h, reward.data_ptr(), done.data_ptr(), values.data_ptr(), 3, T, n, .99, .95, got.data_ptr(), None, torch.cuda.current_stream(DEV).cuda_stream) == 0
+    assert torch.equal(got, want)
