@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import operator
 import os
 
 import torch
@@ -428,7 +429,18 @@ class Pcgrl:
             raise PcgrlError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
         return C.c_void_p(t.data_ptr()), (t.stride(0) if n > 1 else V)
 
+    def _whole(self, v, name):
+        """A number that a 32-bit field holds (ctypes would keep the low bits of any other)."""
+        try:
+            k = operator.index(v)
+        except TypeError:
+            raise PcgrlError(f"{name} must be a whole number, got {v!r}") from None
+        if not 0 <= k < 2**31:
+            raise PcgrlError(f"{name} must be in 0..2^31-1, got {k}")
+        return k
+
     def _sampling(self, logits, uniform, mask, n_rows, temperature, top_k, top_p, min_p):
+        top_k = self._whole(top_k, "top_k")
         how = PcgrlSampling(type=self._type(logits, "logits"), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
         x, how.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
         n, how.n_classes = logits.shape

@@ -27,3 +27,16 @@ def test_factors_beyond_64_bits_are_refused(more):
 def test_large_factors_that_are_numbers_are_not():
     for more in (dict(scale=1e30, temperature=1e-30), dict(scale=1e-300, entropy_coef=1e300), dict(scale=0., entropy_coef=1e300, value_coef=1e300), dict(scale=-1e300)):
         assert policy_loss(n_rows=0, stats=None, **more) == OK
+
+
+@pytest.mark.parametrize("k", [-1, 2**31, 2**32, 2**32 + 5, 10**30, 1.5, "5", None])
+def test_a_top_k_that_is_no_32_bit_number_is_refused(k):
+    """It would be another one in the structure of the C interface (no tensor is looked at before)."""
+    import torch
+    env = object.__new__(binding.Pcgrl)
+    env.device = torch.device("cuda", 0)
+    x = torch.zeros((3, 2))
+    with pytest.raises(binding.PcgrlError, match="top_k"):
+        env._sampling(x, torch.zeros(3), None, None, 1.0, k, 1.0, 0.0)
+    with pytest.raises(binding.PcgrlError, match="logits must be a tensor on"):
+        env._sampling(x, torch.zeros(3), None, None, 1.0, 2**31 - 1, 1.0, 0.0)
