@@ -68,6 +68,7 @@ class PcgrlLoss(C.Structure):
     ]
 
 
+MAX_CLASSES = 32768
 LOSS_STATS = 7  # the loss, rows counted, then sums over them: policy loss, entropy, value loss, divergence, clipped rows
 
 EXPORTS = [
@@ -439,11 +440,16 @@ class Pcgrl:
             raise PcgrlError(f"{name} must be in 0..2^31-1, got {k}")
         return k
 
+    def _classes(self, V):
+        if not 1 <= V <= MAX_CLASSES:
+            raise PcgrlError(f"logits must have 1..{MAX_CLASSES} classes, got {V}")
+        return V
+
     def _sampling(self, logits, uniform, mask, n_rows, temperature, top_k, top_p, min_p):
         top_k = self._whole(top_k, "top_k")
         how = PcgrlSampling(type=self._type(logits, "logits"), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
         x, how.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
-        n, how.n_classes = logits.shape
+        n, how.n_classes = logits.shape[0], self._classes(logits.shape[1])
         if n_rows is not None and n != n_rows:
             raise PcgrlError(f"logits must have a row for each of the {n_rows} environments, got {n}")
         m = None
@@ -508,6 +514,8 @@ class Pcgrl:
         if not isinstance(reward, torch.Tensor) or reward.dim() != 2:
             raise PcgrlError("reward must be a [steps, environments] tensor")
         T, n = shape = tuple(reward.shape)
+        if T > 1 << 20 or n > 1 << 24:
+            raise PcgrlError(f"reward must have at most 2^20 steps of 2^24 environments, got {shape}")
         r = self._dev(reward, torch.float32, shape, "reward")
         d = self._dev(done, torch.bool if getattr(done, "dtype", None) == torch.bool else torch.uint8, shape, "done")
         v = self._dev(values, values.dtype, (T + 1, n), "values")
@@ -537,7 +545,7 @@ class Pcgrl:
         l = PcgrlLoss(type=self._type(logits, "logits"), temperature=temperature, clip_low=clip_low, clip_high=clip_high,
                       entropy_coef=entropy_coef, value_coef=value_coef)
         l.logits, l.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
-        n, V = logits.shape
+        n, V = logits.shape[0], self._classes(logits.shape[1])
         l.n_rows, l.n_classes, l.scale = n, V, 1 / max(n, 1) if scale is None else scale
         if mask is not None:
             l.mask, l.mask_stride = self._rows(mask, (torch.uint8, torch.bool), (n, V), "mask", one_for_all=True)
