@@ -430,6 +430,12 @@ class Pcgrl:
             raise PcgrlError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
         return C.c_void_p(t.data_ptr()), (t.stride(0) if n > 1 else V)
 
+    def _number(self, v, name):
+        try:
+            return C.c_double(v).value
+        except (TypeError, OverflowError):
+            raise PcgrlError(f"{name} must be a number that a double holds, got {type(v).__name__}") from None
+
     def _whole(self, v, name):
         """A number that a 32-bit field holds (ctypes would keep the low bits of any other)."""
         try:
@@ -447,7 +453,8 @@ class Pcgrl:
 
     def _sampling(self, logits, uniform, mask, n_rows, temperature, top_k, top_p, min_p):
         top_k = self._whole(top_k, "top_k")
-        how = PcgrlSampling(type=self._type(logits, "logits"), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+        how = PcgrlSampling(type=self._type(logits, "logits"), temperature=self._number(temperature, "temperature"), top_k=top_k,
+                            top_p=self._number(top_p, "top_p"), min_p=self._number(min_p, "min_p"))
         x, how.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
         n, how.n_classes = logits.shape[0], self._classes(logits.shape[1])
         if n_rows is not None and n != n_rows:
@@ -455,7 +462,7 @@ class Pcgrl:
         m = None
         if mask is not None:
             m, how.mask_stride = self._rows(mask, (torch.uint8, torch.bool), logits.shape, "mask", one_for_all=True)
-        u = self._dev(uniform, torch.float32, (n,), "uniform", optional=temperature == 0)
+        u = self._dev(uniform, torch.float32, (n,), "uniform", optional=how.temperature == 0)
         return how, x, m, u, n
 
     def pcgrl_sample(self, logits, uniform, mask=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, actions=None, log_probs=None):
@@ -511,6 +518,7 @@ class Pcgrl:
                 _check(rc, "pcgrl_advantages")
             return advantages, returns
         code = self._type(values, "values")
+        discount, trace = self._number(discount, "discount"), self._number(trace, "trace")
         if not isinstance(reward, torch.Tensor) or reward.dim() != 2:
             raise PcgrlError("reward must be a [steps, environments] tensor")
         T, n = shape = tuple(reward.shape)
@@ -542,11 +550,12 @@ class Pcgrl:
             if rc:
                 _check(rc, "pcgrl_policy_loss")
             return dict(stats=stats, grad_logits=grad_logits, grad_values=grad_values)
-        l = PcgrlLoss(type=self._type(logits, "logits"), temperature=temperature, clip_low=clip_low, clip_high=clip_high,
-                      entropy_coef=entropy_coef, value_coef=value_coef)
+        f = self._number
+        l = PcgrlLoss(type=self._type(logits, "logits"), temperature=f(temperature, "temperature"), clip_low=f(clip_low, "clip_low"),
+                      clip_high=f(clip_high, "clip_high"), entropy_coef=f(entropy_coef, "entropy_coef"), value_coef=f(value_coef, "value_coef"))
         l.logits, l.logits_stride = self._rows(logits, (logits.dtype,), None, "logits")
         n, V = logits.shape[0], self._classes(logits.shape[1])
-        l.n_rows, l.n_classes, l.scale = n, V, 1 / max(n, 1) if scale is None else scale
+        l.n_rows, l.n_classes, l.scale = n, V, 1 / max(n, 1) if scale is None else f(scale, "scale")
         if mask is not None:
             l.mask, l.mask_stride = self._rows(mask, (torch.uint8, torch.bool), (n, V), "mask", one_for_all=True)
         f32 = torch.float32

@@ -222,7 +222,9 @@ bool mask_rows(PyObject* o, const Env* e, int64_t n, int64_t V, void** out, int6
 bool number(PyObject* o, double* out) {
   if (!PyFloat_Check(o) && !PyLong_Check(o)) return false;
   *out = PyFloat_AsDouble(o);
-  return !(*out == -1. && PyErr_Occurred());
+  if (*out != -1. || !PyErr_Occurred()) return true;
+  PyErr_Clear();  // (a whole number that no double holds)
+  return false;
 }
 // An output: the caller's tensor, or a new one where there is none.
 bool output(PyObject* o, const Env* e, c10::ScalarType type, const int64_t* dims, int nd, at::Tensor* t, void** out) {

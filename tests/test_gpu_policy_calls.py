@@ -43,3 +43,21 @@ def test_sizes_beyond_32_bits(env):
     for T, n in ((2**32 + 3, 0), (2**31, 0), (2**20 + 1, 0)):
         with pytest.raises(binding.PcgrlError):
             env.pcgrl_advantages(e(f32, T, n), e(torch.uint8, T, n), e(f32, T + 1, n), .9, .9)
+
+
+@pytest.mark.parametrize("v", [10**400, "1", None], ids=["large", "text", "none"])
+def test_numbers_that_are_none(env, v):
+    """One that no double holds, and what is no number."""
+    x, u, a = torch.zeros((5, 7), device=DEV), torch.zeros((5,), device=DEV), torch.zeros((5,), dtype=torch.int32, device=DEV)
+    r, d = torch.zeros((4, 3), device=DEV), torch.zeros((4, 3), dtype=torch.uint8, device=DEV)
+    values = torch.zeros((5, 3), device=DEV)
+    bad = pytest.raises(binding.PcgrlError, match="must be a number")
+    for name in ("temperature", "top_p", "min_p"):
+        with bad:
+            env.pcgrl_sample(x, u, **{name: v})
+    for name in ("temperature", "clip_low", "clip_high", "entropy_coef", "value_coef") + (("scale",) if v is not None else ()):
+        with bad:
+            env.pcgrl_policy_loss(x, a, u, **{name: v})
+    for discount, trace in ((v, .9), (.9, v)):
+        with bad:
+            env.pcgrl_advantages(r, d, values, discount, trace)

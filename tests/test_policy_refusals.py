@@ -40,3 +40,14 @@ def test_a_top_k_that_is_no_32_bit_number_is_refused(k):
         env._sampling(x, torch.zeros(3), None, None, 1.0, k, 1.0, 0.0)
     with pytest.raises(binding.PcgrlError, match="logits must be a tensor on"):
         env._sampling(x, torch.zeros(3), None, None, 1.0, 2**31 - 1, 1.0, 0.0)
+
+
+@pytest.mark.parametrize("v", [10**400, -10**400, "1", None, [1.0], 1j], ids=["large", "low", "text", "none", "list", "complex"])
+def test_a_coefficient_that_is_no_number_is_refused(v):
+    import torch
+    env = object.__new__(binding.Pcgrl)
+    env.device = torch.device("cuda", 0)
+    x = torch.zeros((3, 2))
+    for more in ((v, 0, 1.0, 0.0), (1.0, 0, v, 0.0), (1.0, 0, 1.0, v)):
+        with pytest.raises(binding.PcgrlError, match="temperature|top_p|min_p"):
+            env._sampling(x, torch.zeros(3), None, None, *more)
