@@ -430,6 +430,10 @@ class Pcgrl:
             raise PcgrlError(f"{name} must have contiguous rows that do not overlap, got strides {t.stride()}")
         return C.c_void_p(t.data_ptr()), (t.stride(0) if n > 1 else V)
 
+    def _written(self, *tensors):
+        """What a call has written through a pointer has changed for autograd too (tensors of inference mode have no version)."""
+        torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+
     def _number(self, v, name):
         try:
             return C.c_double(v).value
@@ -483,6 +487,7 @@ class Pcgrl:
         a = self._dev(actions, torch.int32, (n,), "actions")
         lp = self._dev(log_probs, torch.float32, (n,), "log_probs")
         _check(self.L.pcgrl_sample(self.h, C.byref(how), x, m, u, n, a, lp, self._st()), "pcgrl_sample")
+        self._written(actions, log_probs)
         return actions, log_probs
 
     def pcgrl_step_logits(self, logits, uniform, obs=None, reward=None, done=None, mask=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
@@ -506,6 +511,7 @@ class Pcgrl:
         r = self._dev(reward, torch.float32, (n,), "reward", optional=True)
         d = self._dev(done, torch.uint8, (n,), "done", optional=True)
         _check(self.L.pcgrl_step_logits(self.h, C.byref(how), x, m, u, a, lp, o, r, d, self._st()), "pcgrl_step_logits")
+        self._written(actions, log_probs, obs, reward, done)
         return actions, log_probs
 
     def pcgrl_advantages(self, reward, done, values, discount, trace, advantages=None, returns=None):
@@ -534,6 +540,7 @@ class Pcgrl:
         a = self._dev(advantages, torch.float32, shape, "advantages")
         q = self._dev(returns, torch.float32, shape, "returns")
         _check(self.L.pcgrl_advantages(self.h, r, d, v, code, T, n, discount, trace, a, q, self._st()), "pcgrl_advantages")
+        self._written(advantages, returns)
         return advantages, returns
 
     def pcgrl_policy_loss(self, logits, actions, advantages, old_log_probs=None, mask=None, values=None, returns=None, temperature=1.0,
@@ -542,7 +549,8 @@ class Pcgrl:
         """The clipped policy loss of logits [n, classes] and its gradients, as a dict: `stats` (LOSS_STATS
         float32), `grad_logits` and, with values, `grad_values`, made here where no tensor is given.  The
         gradients are for logits.backward(grad_logits) or torch.autograd.backward; grad_logits may be
-        the logits.  log_probs and entropies [n] float32 are written if given.  scale: default 1 / n."""
+        the logits if the operation that made them does not need them for its own gradient (a linear layer does not, a
+        tanh or a softmax does, and autograd then says that they have been modified).  log_probs and entropies [n] float32 are written if given.  scale: default 1 / n."""
         got = self._env.policy_loss(logits, actions, advantages, old_log_probs, mask, values, returns, temperature, clip_low, clip_high,
                                     entropy_coef, value_coef, scale, grad_logits, grad_values, log_probs, entropies, stats, workspace)
         if got != _LOOK:
@@ -582,6 +590,7 @@ class Pcgrl:
             raise PcgrlError(f"workspace must hold {size} bytes")
         l.workspace = self._dev(workspace, torch.uint8, tuple(workspace.shape), "workspace")
         _check(self.L.pcgrl_policy_loss(self.h, C.byref(l), self._st()), "pcgrl_policy_loss")
+        self._written(grad_logits, grad_values, log_probs, entropies, stats, workspace)
         return dict(stats=stats, grad_logits=grad_logits, grad_values=grad_values)
 
     def pcgrl_bad_action_count(self) -> int:

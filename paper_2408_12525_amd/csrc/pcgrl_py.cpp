@@ -238,6 +238,14 @@ bool output(PyObject* o, const Env* e, c10::ScalarType type, const int64_t* dims
   return true;
 }
 
+// What a call has written through a pointer has changed for autograd too: a backward pass that has kept it then says so.  (New tensors
+// have not been seen by anybody, and tensors of inference mode have no version.)
+void written(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 struct Draw {
   pcgrl_sampling how;
   void *logits, *mask, *uniform, *actions, *log_probs;
@@ -273,6 +281,8 @@ PyObject* env_sample(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   rc = pcgrl_sample(e->ctx, &d.how, d.logits, static_cast<const uint8_t*>(d.mask), static_cast<const float*>(d.uniform), d.n,
                     static_cast<int32_t*>(d.actions), static_cast<float*>(d.log_probs), st);
   Py_END_ALLOW_THREADS
+  if (rc == PCGRL_OK)
+    for (int i : {7, 8}) written(a[i]);
   return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(d.a), THPVariable_Wrap(d.lp));
 }
 
@@ -291,6 +301,8 @@ PyObject* env_step_logits(PyObject* self, PyObject* const* a, Py_ssize_t n) {
                          static_cast<int32_t*>(d.actions), static_cast<float*>(d.log_probs), static_cast<uint8_t*>(obs),
                          static_cast<float*>(rew), static_cast<uint8_t*>(done), st);
   Py_END_ALLOW_THREADS
+  if (rc == PCGRL_OK)
+    for (int i : {7, 8, 9, 10, 11}) written(a[i]);
   return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(d.a), THPVariable_Wrap(d.lp));
 }
 
@@ -316,6 +328,8 @@ PyObject* env_advantages(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   rc = pcgrl_advantages(e->ctx, static_cast<const float*>(rew), static_cast<const uint8_t*>(done), val, type, (int32_t)shape[0], (int32_t)shape[1],
                         discount, trace, static_cast<float*>(adv), static_cast<float*>(ret), st);
   Py_END_ALLOW_THREADS
+  if (rc == PCGRL_OK)
+    for (int i : {5, 6}) written(a[i]);
   return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(ta), THPVariable_Wrap(tr));
 }
 
@@ -379,6 +393,8 @@ PyObject* env_policy_loss(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Py_BEGIN_ALLOW_THREADS
   rc = pcgrl_policy_loss(e->ctx, &l, st);
   Py_END_ALLOW_THREADS
+  if (rc == PCGRL_OK)
+    for (int i : {13, 14, 15, 16, 17, 18}) written(a[i]);
   PyObject* values = val ? THPVariable_Wrap(tv) : Py_NewRef(Py_None);
   return Py_BuildValue("(iNNN)", rc, THPVariable_Wrap(ts), THPVariable_Wrap(tg), values);
 }

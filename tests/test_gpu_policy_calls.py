@@ -61,3 +61,67 @@ def test_numbers_that_are_none(env, v):
     for discount, trace in ((v, .9), (.9, v)):
         with bad:
             env.pcgrl_advantages(r, d, values, discount, trace)
+
+
+def test_gradients_over_the_logits_where_autograd_needs_them(env):
+    """A head that keeps its output for its own gradient may not find another tensor in its place: autograd says so. One that does
+    not keep it goes on, and so do calls with results of their own."""
+    g = torch.Generator(DEV).manual_seed(3)
+    n, V, d = 60, 9, 16
+    feats = torch.randn((n, d), generator=g, device=DEV)
+    head = torch.randn((d, V), generator=g, device=DEV).mul_(.3).requires_grad_()
+    act, adv = torch.randint(0, V, (n,), generator=g, device=DEV).int(), torch.randn((n,), generator=g, device=DEV)
+    logits = feats @ head
+    logits.backward(env.pcgrl_policy_loss(logits, act, adv)["grad_logits"])
+    want, head.grad = head.grad, None
+    logits = feats @ head
+    logits.backward(env.pcgrl_policy_loss(logits, act, adv, grad_logits=logits)["grad_logits"])
+    assert torch.equal(head.grad, want)
+    kept = torch.tanh(feats @ head)
+    with pytest.raises(binding.PcgrlError):
+        env.pcgrl_policy_loss(kept, act, adv, grad_logits=kept, clip_low=2.)
+    kept.sum().backward()                               # (a refused call writes nothing)
+    kept = torch.tanh(feats @ head)
+    got = env.pcgrl_policy_loss(kept, act, adv, grad_logits=kept)["grad_logits"]
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.backward(got)
+    values = torch.tanh(feats @ head[:, 0])
+    got = env.pcgrl_policy_loss((feats @ head).detach(), act, adv, values=values, returns=adv, grad_values=values)["grad_values"]
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        values.backward(got)
+
+
+def test_what_a_call_writes_counts_as_changed(env):
+    """Every tensor of the caller's that a call writes, and none that it reads; through both call paths."""
+    n, V, T = 20, 5, 6
+    f = lambda *s: torch.zeros(s, device=DEV)  # noqa: E731
+    x, u, a, lp = torch.randn((n, V), device=DEV), torch.rand((n,), device=DEV), torch.zeros((n,), dtype=torch.int32, device=DEV), f(n)
+    steps = dict(reward=f(T, n), done=torch.zeros((T, n), dtype=torch.uint8, device=DEV), values=f(T + 1, n))
+    outs = dict(grad_logits=f(n, V), grad_values=f(n), log_probs=f(n), entropies=f(n), stats=f(7), workspace=torch.zeros((1 << 20,), dtype=torch.uint8, device=DEV))
+    adv, ret, values = f(T, n), f(T, n), f(n)
+
+    class Float:                                        # (a number that the compiled path leaves to Python)
+        def __float__(self):
+            return 1.0
+
+    for one in (1.0, Float()):
+        for call, written, read in ((lambda: env.pcgrl_sample(x, u, temperature=one, actions=a, log_probs=lp), [a, lp], [x, u]),
+                                    (lambda: env.pcgrl_advantages(*steps.values(), one, .9, advantages=adv, returns=ret), [adv, ret], list(steps.values())),
+                                    (lambda: env.pcgrl_policy_loss(x, a, u, old_log_probs=lp, values=values, returns=u, temperature=one, **outs), list(outs.values()), [x, a, u, lp, values])):
+            before = [t._version for t in written], [t._version for t in read]
+            call()
+            assert all(t._version > v for t, v in zip(written, before[0])) and [t._version for t in read] == before[1]
+    with torch.inference_mode():
+        y, b = torch.randn((n, V), device=DEV), torch.zeros((n,), dtype=torch.int32, device=DEV)
+    env.pcgrl_sample(y, u, actions=b)                   # (those have no version)
+    env.pcgrl_policy_loss(y, b, u, grad_logits=y)
+
+
+def test_a_step_counts_as_a_change_of_its_actions():
+    e = binding.Pcgrl(wl.workload("dungeon32", batch=8), 0)
+    e.pcgrl_reset(1)
+    x, u, a, lp = torch.zeros((8, 7), device=DEV), torch.rand((8,), device=DEV), torch.zeros((8,), dtype=torch.int32, device=DEV), torch.zeros((8,), device=DEV)
+    before = a._version, lp._version
+    e.pcgrl_step_logits(x, u, actions=a, log_probs=lp)
+    assert a._version > before[0] and lp._version > before[1]
+    e.close()
