@@ -392,7 +392,7 @@ typedef struct {
   const int32_t* actions;      /* [n_rows]; a row whose action is no class that may be chosen is not counted */
   const float* advantages;     /* [n_rows] */
   const float* old_log_probs;  /* [n_rows] of the policy that acted, or NULL: no ratio, nothing is clipped */
-  const void* values;          /* [n_rows], or NULL: no value loss */
+  const void* values;          /* [n_rows], or NULL: no value loss; required with grad_values */
   const float* returns;        /* [n_rows], required with values */
   double temperature;          /* 1e-30 .. 3e38 */
   double clip_low, clip_high;  /* the ratio is clipped to [1 - clip_low, 1 + clip_high]; 0..1 and >= 0 */

@@ -277,6 +277,7 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
         misaligned(l->values, size) || misaligned(l->returns, 4) || misaligned(l->grad_logits, size) || misaligned(l->grad_values, size) ||
         misaligned(l->log_probs, 4) || misaligned(l->entropies, 4))
       return PCGRL_E_CONFIG;
+    if (l->grad_values && !l->values) return PCGRL_E_NULL;
     if (bad_rows(l->n_rows, l->logits_stride, l->n_classes)) return PCGRL_E_CONFIG;
     if (l->mask && l->mask_stride != 0 && bad_rows(l->n_rows, l->mask_stride, l->n_classes)) return PCGRL_E_CONFIG;
     if (l->grad_logits && bad_rows(l->n_rows, l->grad_stride, l->n_classes)) return PCGRL_E_CONFIG;
@@ -287,7 +288,7 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
     const Memory in[] = {{in_place ? nullptr : l->logits, logits}, {l->mask, span(n, l->mask_stride, l->n_classes, 1)},
                          {l->actions, row}, {l->advantages, row}, {l->old_log_probs, row},
                          {l->grad_values == l->values ? nullptr : l->values, value}, {l->values ? l->returns : nullptr, row}};
-    const Memory out[] = {{l->grad_logits, span(n, l->grad_stride, l->n_classes, size)}, {l->values ? l->grad_values : nullptr, value}, {l->log_probs, row},
+    const Memory out[] = {{l->grad_logits, span(n, l->grad_stride, l->n_classes, size)}, {l->grad_values, value}, {l->log_probs, row},
                           {l->entropies, row}, {l->stats, PCGRL_LOSS_STATS * 4}, {l->stats ? l->workspace : nullptr, (size_t)pcgrl_policy_loss_workspace()}};
     if (any_overlap(out, in)) return PCGRL_E_CONFIG;
   }
@@ -303,7 +304,7 @@ int pcgrl_policy_loss(const pcgrl_ctx* ctx, const pcgrl_loss* l, void* stream) {
   a.values = l->values;
   a.returns = l->returns;
   a.grad_logits = l->grad_logits;
-  a.grad_values = l->values ? l->grad_values : nullptr;
+  a.grad_values = l->grad_values;
   a.log_probs = l->log_probs;
   a.entropies = l->entropies;
   a.partial = l->stats ? static_cast<double*>(l->workspace) : nullptr;

@@ -125,3 +125,9 @@ def test_a_step_counts_as_a_change_of_its_actions():
     e.pcgrl_step_logits(x, u, actions=a, log_probs=lp)
     assert a._version > before[0] and lp._version > before[1]
     e.close()
+
+
+def test_a_gradient_of_values_needs_values(env):
+    x, a, adv = torch.zeros((5, 7), device=DEV), torch.zeros((5,), dtype=torch.int32, device=DEV), torch.zeros((5,), device=DEV)
+    with pytest.raises(binding.PcgrlError):
+        env.pcgrl_policy_loss(x, a, adv, grad_values=torch.zeros((5,), device=DEV))

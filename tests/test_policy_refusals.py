@@ -51,3 +51,9 @@ def test_a_coefficient_that_is_no_number_is_refused(v):
     for more in ((v, 0, 1.0, 0.0), (1.0, 0, v, 0.0), (1.0, 0, 1.0, v)):
         with pytest.raises(binding.PcgrlError, match="temperature|top_p|min_p"):
             env._sampling(x, torch.zeros(3), None, None, *more)
+
+
+@pytest.mark.parametrize("rc,more", [(NULL, dict(grad_values=6 * P)), (CONFIG, dict(grad_values=6 * P + 2)), (OK, dict(n_rows=0, stats=None, grad_values=6 * P))])
+def test_a_gradient_of_values_needs_values(rc, more):
+    """It would be left as it was."""
+    assert policy_loss(**more) == rc
