@@ -359,7 +359,8 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
 /* pcgrl_sample for every environment, and pcgrl_step with the actions drawn: a step of a policy in the
  * loop as one call (Methods / Training).  n_classes must be the number of tile types, n_rows is the
  * batch; actions is required (and written), log_probs, obs, reward and done may be NULL.
- * Errors: those of both (what pcgrl_step refuses is refused after the actions have been drawn). */
+ * Errors: those of both (what pcgrl_step refuses is refused after the actions have been drawn), and E_CONFIG if actions or
+ * log_probs overlap obs, reward or done. */
 int pcgrl_step_logits(pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* logits, const uint8_t* mask,
                       const float* uniform, int32_t* actions, float* log_probs, uint8_t* obs, float* reward,
                       uint8_t* done, void* stream);

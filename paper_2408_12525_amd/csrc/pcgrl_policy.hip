@@ -221,6 +221,12 @@ int pcgrl_step_logits(pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* log
                       int32_t* actions, float* log_probs, uint8_t* obs, float* reward, uint8_t* done, void* stream) {
   if (!ctx || !how) return PCGRL_E_NULL;
   if (how->n_classes != tiles_in(ctx)) return PCGRL_E_CONFIG;
+  // (the step reads actions while it writes, and would write over the log-probabilities)
+  const size_t n = (size_t)levels_of(ctx);
+  const Memory drawn[] = {{actions, n * 4}, {log_probs, n * 4}}, stepped[] = {{obs, n * (size_t)pcgrl_obs_stride(ctx)}, {reward, n * 4}, {done, n}};
+  for (const Memory& d : drawn)
+    for (const Memory& s : stepped)
+      if (overlap(d.at, d.bytes, s.at, s.bytes)) return PCGRL_E_CONFIG;
   const int rc = pcgrl_sample(ctx, how, logits, mask, uniform, levels_of(ctx), actions, log_probs, stream);
   return rc == PCGRL_OK ? pcgrl_step(ctx, actions, obs, reward, done, stream) : rc;
 }

@@ -131,3 +131,30 @@ def test_a_gradient_of_values_needs_values(env):
     x, a, adv = torch.zeros((5, 7), device=DEV), torch.zeros((5,), dtype=torch.int32, device=DEV), torch.zeros((5,), device=DEV)
     with pytest.raises(binding.PcgrlError):
         env.pcgrl_policy_loss(x, a, adv, grad_values=torch.zeros((5,), device=DEV))
+
+
+def test_step_logits_refuses_outputs_in_one_place():
+    """The step would read actions where it writes; what the draw reads may be written by the step."""
+    e, other = (binding.Pcgrl(wl.workload("dungeon32", batch=40), 0) for _ in range(2))
+    size = math.prod(e.obs_shape)
+    room = torch.zeros((size,), dtype=torch.uint8, device=DEV)
+    g = torch.Generator(DEV).manual_seed(1)
+    x, u = torch.randn((40, e.K), generator=g, device=DEV), torch.rand((40,), generator=g, device=DEV)
+    for one in (e, other):
+        one.pcgrl_reset(5)
+    obs, at = room.view(e.obs_shape), (size - 160) // 4 * 4
+    inside = room[at:at + 160]
+    f = lambda n=40: torch.zeros((n,), device=DEV)  # noqa: E731
+    ints, floats, flags = inside.view(torch.int32), inside.view(torch.float32), inside[:40]
+    wide = f(60)
+    for more in (dict(obs=obs, actions=ints), dict(obs=obs, log_probs=floats), dict(reward=floats, actions=ints), dict(done=flags, actions=ints), dict(done=inside[120:], log_probs=floats),
+                 dict(reward=wide[20:], log_probs=wide[:40])):
+        with pytest.raises(binding.PcgrlError, match="configuration field"):
+            e.pcgrl_step_logits(x, u, **more)
+    reward, done = f(), torch.zeros((40,), dtype=torch.uint8, device=DEV)
+    want = e.pcgrl_step_logits(x, u, obs, reward, done)
+    got = other.pcgrl_step_logits(x, u, reward=u)       # (the numbers have been read by then)
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and torch.equal(u, reward)
+    assert torch.equal(other.pcgrl_observe(), obs)
+    for one in (e, other):
+        one.close()
