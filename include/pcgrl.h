@@ -339,8 +339,8 @@ typedef struct {
  * logit, equal ones by index, a class is kept while it is among the first top_k, while the sum of the
  * weights before it is below top_p times the sum of what top_k left, and while w >= min_p.  The
  * action is the first kept class, by index, at which the running sum of the kept weights exceeds
- * uniform times their sum; weights are rounded to the nearest multiple of 2^-38 of the largest, and summed
- * exactly.
+ * uniform times their sum; weights are rounded to multiples of 2^-50 of the largest for up to 8 classes, 2^-47 up to 64, 2^-42 up
+ * to 2048, then of one bit less for each doubling, to 2^-38 (off by at most 0.7 of them), and summed exactly.
  *   logits   : device, [n_rows][logits_stride] elements
  *   mask     : device, uint8 [n_rows][mask_stride], or NULL
  *   uniform  : device, float32 [n_rows] in [0, 1) (what is outside or NaN counts as the nearest such number,

@@ -162,10 +162,13 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
   a.top_k = how->top_k < how->n_classes ? how->top_k : 0;
   a.inv_temperature = best ? 0. : 1. / how->temperature;
   a.slope = 64. * 1.44269504088896340736 * a.inv_temperature;
-  a.reach = (float)(40. * 0.69314718055994530942 * how->temperature);
+  const int bits = weight_bits(a.n);
+  a.unit = std::ldexp(1., bits);
+  a.inv_unit = std::ldexp(1., -bits);
+  a.reach = (float)((bits + 2) * 0.69314718055994530942 * how->temperature);
   a.top_p = how->top_p;
-  a.min_p = how->min_p;
-  const bool cut = a.top_k > 0 || a.top_p < 1. || a.min_p > 0.;
+  a.least = how->min_p * a.unit;
+  const bool cut = a.top_k > 0 || a.top_p < 1. || a.least > 0.;
   hipStream_t st = static_cast<hipStream_t>(stream);
   return by_type(how->type, [&](auto type) {
     using T = decltype(type);

@@ -234,29 +234,31 @@ template <int TEAM> struct Team {
   }
 };
 
-// Powers of two by a table of 2^(i / 64), 64 doubles in LDS, times `unit`: power() is unit * 2^(z / 64) to 2^-44, with four terms
-// of the series of what is left of z, 17 instructions.
+// Powers of two by a table of 2^(i / 64), 64 doubles in LDS, times `unit`: power() is unit * 2^(z / 64) to 2^-44 (what the fifth term
+// could add, (ln(2) / 128)^5 / 120), with four terms of the series of what is left of z, 17 instructions; with five to 2^-51.
 template <int TEAM> __device__ __forceinline__ void fill_powers(double* table, double unit) {
   if (threadIdx.x < 64) table[threadIdx.x] = unit * 2. * pow2((double)threadIdx.x / 64. - 1.);
   if (TEAM <= 64) __syncthreads();  // (larger teams have a barrier for their largest logit before they read it)
 }
-__device__ __forceinline__ double power_from(const double* table, double z) {  // (z >= -64000, or NaN)
+template <int TERMS = 4> __device__ __forceinline__ double power_from(const double* table, double z) {  // (z >= -64000, or NaN)
   const double t = z + 0x1.8p52, r = z - (t - 0x1.8p52);  // the nearest whole number, in the low word of t
   const int n = __double2loint(t);
   double q = 5.732851688640402e-10;                       // (ln(2) / 64)^4 / 4!
+  if constexpr (TERMS == 5) q = __builtin_fma(1.2417843701716925e-12, r, q);  // 5
   q = __builtin_fma(q, r, 2.1173137155464774e-07);        // 3
   q = __builtin_fma(q, r, 5.864904955056169e-05);         // 2
   q = __builtin_fma(q, r, 0.010830424696249145) * r;      // 1
   const double of = table[n & 63];
   return __builtin_ldexp(__builtin_fma(of, q, of), n >> 6);
 }
-__device__ __forceinline__ double power(const double* table, double z) { return power_from(table, __builtin_fmax(z, -64000.)); }
+template <int TERMS = 4> __device__ __forceinline__ double power(const double* table, double z) { return power_from<TERMS>(table, __builtin_fmax(z, -64000.)); }
 
-// The natural logarithm of v >= 1 (NaN for infinity and NaN), to about 2^-44, with `table` times 1 / `unit`: what the one in
-// single precision leaves, some 1e-7, by the series.  The library's takes a hundred registers of constants out of a loop.
-__device__ __forceinline__ double log_of(const double* table, double unit, double v) {
+// The natural logarithm of v >= 1 (NaN for infinity and NaN), to about 2^-44, with `inv_unit` one over the table's unit: what the one in
+// single precision leaves, some 1e-7, by the series.  The library's takes a hundred registers of constants out of a loop.  It goes into
+// log-probabilities, which are float32, and into the ratio to such a one: 2^-24 of them is what there is.
+__device__ __forceinline__ double log_of(const double* table, double inv_unit, double v) {
   const double about = (double)__builtin_amdgcn_logf((float)v);
-  const double rest = v * (power(table, -64. * about) * (1. / unit)) - 1.;
+  const double rest = v * (power(table, -64. * about) * inv_unit) - 1.;
   return __builtin_fma(about, 0.69314718055994530942, rest - .5 * rest * rest);
 }
 
@@ -383,15 +385,23 @@ struct SampleArgs {
   int32_t n, top_k;     // (top_k: 0 or 1..n-1)
   double slope;         // 64 * log2(e) / temperature
   float reach;          // below the largest logit by more than this there are no weights
-  double inv_temperature, top_p, min_p;
+  double inv_temperature, top_p, least;  // least: min_p, as a weight
+  double unit, inv_unit;  // the largest weight, 2^weight_bits(n)
   uint32_t lds_row;     // bytes of LDS that a row takes
 };
 
 constexpr int kSampleBest = 0, kSamplePlain = 1, kSampleCut = 2;
 
-// Weights are held as whole numbers of 2^-38 of the largest one in doubles: the sums of up to 2^15 of them stay below 2^53 and are
+// Weights are held in doubles as whole numbers, the largest as 2^weight_bits(n): the sums of n of them do not exceed 2^53 and are
 // exact, whatever their order, so that a running sum cut up over lanes and wavefronts is the same number as the sum of the parts.
-constexpr double kUnit = 0x1p38;
+// Up to 64 classes that is the only bound (2^50 for 8 classes, 2^47 for 64), and powers have the fifth term for it.  Beyond, where
+// instructions a class are what a draw costs, powers to 2^-44 are good for 2^42; from 2048 classes the sums bind again, to 2^38 for 32 768.
+__host__ __device__ constexpr int weight_bits(int n) {
+  int sums = 53;
+  while ((1 << (53 - sums)) < n) --sums;
+  return n <= 8 ? 50 : n <= 64 ? 47 : sums < 42 ? sums : 42;
+}
+static_assert(weight_bits(8) == 50 && weight_bits(64) == 47 && weight_bits(1000) == 42 && weight_bits(4097) == 40 && weight_bits(PCGRL_MAX_CLASSES) == 38, "");
 
 // The last of the classes that top_k and top_p keep, in the order of falling logits and rising indices.
 struct Cutoff {
@@ -400,18 +410,18 @@ struct Cutoff {
 };
 
 // How a row's weights follow from its logits.
-struct Weigh {
+template <int TERMS> struct Weigh {
   const double* table;
   float top;
   double slope;
-  __device__ __forceinline__ double operator()(float x) const { return __builtin_rint(power(table, ((double)x - (double)top) * slope)); }
+  __device__ __forceinline__ double operator()(float x) const { return __builtin_rint(power<TERMS>(table, ((double)x - (double)top) * slope)); }
 };
 // (the two zeros are equal)
 template <typename T> __device__ __forceinline__ uint32_t class_key(float x) { return key_of(x + 0.f) >> T::kKeyShift; }
 
 __device__ __forceinline__ void put_draw(const SampleArgs& a, int64_t row, int action, float logit, float top, double whole, const double* table) {
   a.actions[row] = action;
-  if (a.log_probs) a.log_probs[row] = (float)(((double)logit - (double)top) * a.inv_temperature - log_of(table, kUnit, whole / kUnit));
+  if (a.log_probs) a.log_probs[row] = (float)(((double)logit - (double)top) * a.inv_temperature - log_of(table, a.inv_unit, whole * a.inv_unit));
 }
 __device__ __forceinline__ void put_nothing(const SampleArgs& a, int64_t row, float top) {
   a.actions[row] = -1;
@@ -563,7 +573,7 @@ __device__ __forceinline__ Cutoff cut_by_halves(const float (&x)[PER], const dou
 }
 
 // Draws of few classes, a row in the registers of one lane, of eight or of sixteen.  With w = 2^((x - top) / (temperature ln 2)), as
-// whole multiples of 2^-38 in doubles, every sum of up to 2^15 of them is exact: the order in which threads add them up does not
+// whole numbers in doubles, every sum of them is exact (weight_bits): the order in which threads add them up does not
 // matter, and an action depends on the numbers given alone.  A row is read once; then come the largest logit, the weights
 // and their sum, the cutoff, what is kept, and the running sum to the target.  One lane holds up to 8 classes: a
 // reduction over lanes is a dozen instructions for each row, and none of these need any; it finds each class's place by
@@ -576,7 +586,7 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(2
   constexpr int kTeams = 256 / TEAM;
   __shared__ double table[64];
   Team<TEAM> team{nullptr};
-  fill_powers<TEAM>(table, kUnit);
+  fill_powers<TEAM>(table, a.unit);
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
     const int rank = team.rank_anew();
     const R of(rank, a.n);
@@ -594,7 +604,7 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(2
       if (rank == 0) put_nothing(a, row, top);
       continue;
     }
-    const Weigh weigh{table, top, a.slope};
+    const Weigh<TEAM * PER <= 64 ? 5 : 4> weigh{table, top, a.slope};
     double w[PER], whole = 0.;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -613,7 +623,7 @@ template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(2
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         const uint32_t key = class_key<T>(x[j]);
-        w[j] = (key > cut.key || (key == cut.key && of.at(j / R::VEC, j % R::VEC) <= cut.index)) && w[j] >= a.min_p * kUnit ? w[j] : 0.;
+        w[j] = (key > cut.key || (key == cut.key && of.at(j / R::VEC, j % R::VEC) <= cut.index)) && w[j] >= a.least ? w[j] : 0.;
         kept += w[j];
       }
       kept = team.sum(kept);
@@ -886,7 +896,7 @@ template <int TEAM> struct BinSums {
 // row, whatever the types.  A bin with more classes than the list holds is binned again by itself, unless they are
 // all equal: then they are counted off by index.
 template <typename T, int TEAM>
-__device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const Weigh& weigh, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double whole,
+__device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const Weigh<4>& weigh, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double whole,
                                               float low, float scale) {
   using C = CutRoom<TEAM>;
   constexpr int kOwn = C::kBins / TEAM;
@@ -1003,7 +1013,7 @@ __device__ __forceinline__ Cutoff cut_by_bins(const Stretch<T, TEAM>& in, const 
 // of this thread's classes is kept outside that bin, m.extra to what each wavefront has in it.  False if the list does not
 // hold the bin.
 template <typename T, int TEAM>
-__device__ __forceinline__ bool share_by_bins(const Stretch<T, TEAM>& in, const Weigh& weigh, Team<TEAM>& team, CutRoom<TEAM>& m, double share, double least, float scale,
+__device__ __forceinline__ bool share_by_bins(const Stretch<T, TEAM>& in, const Weigh<4>& weigh, Team<TEAM>& team, CutRoom<TEAM>& m, double share, double least, float scale,
                                               double& mine) {
   using C = CutRoom<TEAM>;
   constexpr int kOwn = C::kBins / TEAM;
@@ -1051,7 +1061,7 @@ __device__ __forceinline__ bool share_by_bins(const Stretch<T, TEAM>& in, const 
 // For a top_k that the list holds, with the rest of the bin that it ends in: every class that may be kept is listed, ranked once by its
 // logit, for top_k and top_p, and once by its index, for the draw.  False if the list does not hold them, or if top_k keeps all.
 template <typename T, int TEAM>
-__device__ __forceinline__ bool draw_from_list(const Stretch<T, TEAM>& in, const Weigh& weigh, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double least,
+__device__ __forceinline__ bool draw_from_list(const Stretch<T, TEAM>& in, const Weigh<4>& weigh, Team<TEAM>& team, const SampleArgs& a, CutRoom<TEAM>& m, double least,
                                                float scale, double whole, int64_t row) {
   using C = CutRoom<TEAM>;
   constexpr int kOwn = C::kBins / TEAM, kMost = C::kList < TEAM ? C::kList : TEAM;
@@ -1120,7 +1130,7 @@ template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block
   __shared__ CutRoom<TEAM> cut_room[HOW == kSampleCut ? kTeams : 1];
   Team<TEAM> team{room};
   CutRoom<TEAM>& m = cut_room[HOW == kSampleCut ? threadIdx.x / TEAM % kTeams : 0];
-  fill_powers<TEAM>(table, kUnit);
+  fill_powers<TEAM>(table, a.unit);
   __shared__ typename S::Search search;
   const bool searched = HOW == kSampleCut && (a.top_k > 0 || a.top_p < 1.);
   for (int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TEAM; row < a.n_rows; row += (int64_t)gridDim.x * kTeams) {
@@ -1145,7 +1155,7 @@ template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block
       if (rank == 0) put_nothing(a, row, top);
       continue;
     }
-    const Weigh weigh{table, top, a.slope};
+    const Weigh<4> weigh{table, top, a.slope};
     const float range = __builtin_fminf(top - low, a.reach), scale = HOW == kSampleCut && range > 0.f ? (float)CutRoom<TEAM>::kBins / range : 0.f;
     double mine = 0., before, here;
     in.each([&](float x, int) {
@@ -1162,7 +1172,7 @@ template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block
     });
     const double whole = team.sum(mine, before, here);
     double kept = whole;
-    const double least = HOW == kSampleCut ? a.min_p * kUnit : 0.;
+    const double least = HOW == kSampleCut ? a.least : 0.;
     Cutoff cut{0, 0x7fffffff};
     // what is kept of a class's weight
     auto kept_of = [&](float x, int index) {

@@ -309,3 +309,48 @@ def test_advantages_without_returns(env, T, n):
     got = torch.full((T, n), 5., device=DEV)
     assert L.pcgrl_advantages(env.h, reward.data_ptr(), done.data_ptr(), values.data_ptr(), 3, T, n, .99, .95, got.data_ptr(), None, torch.cuda.current_stream(DEV).cuda_stream) == 0
     assert torch.equal(got, want)
+
+
+def weight_bits(V):
+    """Weights are multiples of 2^-this of the largest one, by the number of classes."""
+    return 50 if V <= 8 else 47 if V <= 64 else min(42, 53 - math.ceil(math.log2(V)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [2, 3, 4, 7, 8, 9, 33, 64, 65, 200, 512, 513, 1000, 1024, 2048, 4096, 5000])
+def test_rare_classes_are_drawn_as_often_as_their_weights_say(env, V, dtype):
+    """The first class has a weight of some 2^-20, 2^-30, 2^-36 of the others', which small uniform numbers resolve: numbers 2 % from
+    its border on either side tell it from the next.  A weight is off by at most 0.7 steps: the border by that many, and by V as
+    many in the sum of the others, which is far less of it.  Down to weights of 2^-43 where the steps are that fine."""
+    rng = np.random.default_rng(V)
+    for far in (20, 30, 36, 39, 43):
+        if .7 * 2.**(far + 1 - weight_bits(V)) > .015:
+            continue
+        n = 64
+        x = gpu(np.zeros((n, V)), torch.float64)
+        x[:, 0] = gpu(-far * math.log(2) + rng.random(n) * .6 - .3)
+        x = x.to(TYPES[dtype])
+        w = np.exp(wide64(x)[:, 0])
+        border = w / (w + V - 1)
+        u = np.where(rng.random(n) < .5, border * .98, border * 1.02).astype(np.float32)
+        for how in (dict(), dict(top_p=1 - 2.**-50), dict(top_k=V)):
+            # (a top_p below 1 by 2^-50 keeps the first class, which comes last in its order, only where it has more than that share)
+            if "top_p" in how and not 2.**-far > V * 2.**-48:
+                continue
+            got = env.pcgrl_sample(x, gpu(u), **how)[0].cpu().numpy()
+            assert np.array_equal(got, np.where(u < border, 0, 1)), (far, how)
+
+
+@pytest.mark.parametrize("V", [2, 5, 8, 30, 64, 100, 500, 900])
+def test_actions_to_the_last_bits_of_the_weights(env, V):
+    """Targets as near to borders as uniform numbers of 32 bits come near 0, against the plain statement."""
+    rng, n = np.random.default_rng(V), 300
+    x = gpu(rng.normal(size=(n, V)) * 3, torch.float32)
+    x[:, :V // 2] -= gpu(rng.random((n, 1)) * 25, torch.float32)
+    p = np.exp(wide64(x) - wide64(x).max(1, keepdims=True))
+    borders = (p.cumsum(1) / p.sum(1, keepdims=True))[:, :V // 2]
+    u = (borders[np.arange(n), rng.integers(0, V // 2, n)] * (1 + rng.normal(size=n) * 1e-5)).astype(np.float32)
+    got = env.pcgrl_sample(x, gpu(u))[0].cpu().numpy()
+    want, _, room = policy_oracle.sample(wide64(x), None, u)
+    sure = room > V * (2.**-weight_bits(V) + 2.**-50)   # (0.7 steps a weight; the plain statement's own sums)
+    assert sure.mean() > .3 and np.array_equal(got[sure], want[sure])
