@@ -801,17 +801,14 @@ template <typename T, int TEAM> struct Stretch {
   // pieces) with top_p 101 / 90, without 39 / 36, 1000 of 8000 (4) 14.7 / 13.4, but 2000 of 4000 (2) 15.6 / 16.7, of 2000 (1) 10.8 / 12.0.
   __device__ __forceinline__ bool many_pieces() const { return TEAM > 64 && all > 2 * W; }
   struct Search {
-    double before, sums[16];  // of the wavefront's pieces, at most 8
-    int wave;                 // -1 at the start
+    double sums[16];  // of the wavefront's pieces, at most 8
+    int wave;         // -1 at the start
   };
   template <typename V, typename F>
   __device__ __forceinline__ void find_together(Team<TEAM>& team, Search& search, double before, double here, double target, V value, F found) const {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const bool mine = before <= target && target < before + here;
-    if (mine && lane == 0) {
-      search.wave = wave;
-      search.before = before;
-    }
+    if (mine && lane == 0) search.wave = wave;
     team.sync();
     const int who = __builtin_amdgcn_readfirstlane(search.wave);
     const int from = who * all / W, count = who < 0 ? 0 : (who + 1) * all / W - from;
