@@ -53,8 +53,8 @@ template <typename F> int by_type(int type, F&& f) {
   return f(BF16{});
 }
 // (up to 8 classes: a lane that holds exactly as many.  Beyond that as many lanes as have 8 to 32 classes each: what a row costs besides
-// its classes is shared by the rows of a wavefront.  Measured, us for losses: 20 000 rows of 500 in a wavefront / sixteen lanes 38 / 25, 5000 of 2000 in 256
-// threads / a wavefront 33 / 25, 3000 of 4000 in 256 / 128 32 / 28.5.)
+// its classes is shared by the rows of a wavefront.  Measured, us for losses: 20 000 rows of 500 in a wavefront / sixteen lanes 30 / 21, 5000 of 2000 in 256
+// threads / a wavefront 28 / 19, 3000 of 4000 in 256 / 128 26 / 22.)
 template <typename F> int by_few_classes(int n, F&& f) {
   switch (n) {
     case 1: return f(Shape<1, 1>{});
@@ -81,8 +81,8 @@ template <typename F> int by_classes(int n, F&& f) {
   return f(Shape<1024, 32>{});
 }
 // Workgroups of a loss that the machine holds at once, each of which then takes several rows: four wavefronts a SIMD, five of
-// the smallest teams.  Measured, us for 512 / 1024 / 1280 / 2048 workgroups: 2 097 152 rows of 7 classes 57 / 46 / 45 / 48 (before other steps), 20 000 of
-// 500 25 / 24 / 26 / 26, 1024 of 16 384 33 / 36 / 36 / 36.
+// the smallest teams.  Measured, us for 512 / 1024 / 1280 / 2048 workgroups: 2 097 152 rows of 7 classes 47 / 37 / 35 / 35, 300 000 of 50
+// 62 / 46 / 44 / 43, 20 000 of 500 23 / 20 / 21 / 21; for 256 / 512 / 1024 (of 512 threads) 1024 of 16 384 42 / 31.5 / 32.
 template <int TEAM> constexpr int64_t resident() {
   constexpr int64_t most = (TEAM <= 8 ? 5 : 4) * (int64_t)65536 / team_block<TEAM>();
   static_assert(most <= kLossBlocks, "");
@@ -191,9 +191,9 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
     if (a.n <= 8) return by_few_classes(a.n, either);
     if (a.n <= 64) return either(Shape<8, 8>{});
     // Beyond that, registers for plain draws and where there are enough rows to hide the steps of the halving behind each other, LDS
-    // for the rest.  Measured, us for registers / LDS: 4096 rows of 200 classes in bfloat16 3.8 / 7.6, with top_p 13 / 15, with top_k
-    // and top_p 16 / 23; in float32, with its twice as many bits, with top_p 13 / 10, 60 000 rows 88 / 103; 16 rows 12 / 6.6; 60 000 rows of
-    // 500 in bfloat16 34 / 75, with top_p 201 / 171.
+    // for the rest.  Measured, us for registers / LDS: 4096 rows of 200 classes in bfloat16 3.7 / 7.4, with top_p 12.2 / 15.2, with top_k
+    // and top_p 15.0 / 13.6; in float32, with its twice as many bits, with top_p 12.8 / 10.1, 60 000 rows 88 / 106; 16 rows 11.0 / 9.3; 60 000 rows of
+    // 500 in bfloat16 35 / 76, with top_p 201 / 169.
     if (cut ? a.n <= 256 && n_rows >= (sizeof(typename T::raw) == 2 ? 2048 : 8192) : a.n <= 512) {
       if (a.n <= 128) return either(Shape<8, 16>{});
       if (a.n <= 256) return either(Shape<16, 16>{});
@@ -208,14 +208,14 @@ int pcgrl_sample(const pcgrl_ctx* ctx, const pcgrl_sampling* how, const void* lo
       hipLaunchKernelGGL(kernel, dim3(groups_for<S::kTeam>(n_rows, 1 << 20)), dim3(team_block<S::kTeam>()), lds, st, a);
       return launched();
     };
-    // A wavefront a row where it is short; a workgroup of 256 or 512 threads, of which a compute unit has room for more than one,
-    // or, for a few long rows, of 1024.  Measured, us for 64 / 256 / 512 / 1024 threads a row: 4096 rows of 1024 classes
-    // with top_p 22 / 41 / 80 / 184, 2000 of 4000 44 / 39 / 50 / 113, 1000 of 8000 - / 37 / 39 / 60, 1024 of 28 672 - / 148 / 103 / 135, 300 of
-    // 28 672 in float32 - / 118 / 72 / 59, one of 28 672 - / 50 / 35 / 31.
+    // A wavefront a row where it is short; then a workgroup of 256 or 512 threads, of which a compute unit has room for more than one,
+    // 512 where there are no more than two rows for each of them; 1024 where one row is as much LDS as there is, and for the longest of
+    // rows that have a compute unit each.  Measured, us for 64 / 256 / 512 / 1024 threads a row, with top_p: 4096 rows of 1024 classes 22 /
+    // 41 / 82 / 189, 2000 of 4000 47 / 39 / 51 / 115, 1000 of 8000 - / 33 / 39 / 61, 512 of 8000 - / 25 / 22 / 31, 257 of 12 000 - / 32 / 25 / 39,
+    // 1024 of 28 672 - / 137 / 91 / 131, 257 - / 64 / 45 / 62, 256 - / 59 / 36 / 34; in float32 256 of 28 672 - / - / 33 / 28, 512 - / - / 67 / 57.
     if (a.n <= 1024) return many(Shape<64, 1>{});
-    if (n_rows <= 384 && a.n > 4096) return many(Shape<1024, 1>{});
-    if (a.n <= 8192) return many(Shape<256, 1>{});
-    if (a.n * (int)sizeof(typename T::raw) > 61440) return many(Shape<1024, 1>{});  // (one row is as much LDS as there is)
+    if (a.n * (int)sizeof(typename T::raw) > 61440 || (n_rows <= 256 && a.n > 16384)) return many(Shape<1024, 1>{});
+    if (a.n <= 4096 || (a.n <= 8192 && n_rows > 512)) return many(Shape<256, 1>{});
     return many(Shape<512, 1>{});
   });
 }
