@@ -318,7 +318,8 @@ int pcgrl_unpack_obs(const pcgrl_ctx* ctx, const uint8_t* packed, void* out, int
  * PCGRL_UNPACK_F16 / _BF16 / _F32.  Every array is aligned to its element size.  Numbers of rows and strides are below 2^31.
  *
  * Logits have one row for each decision and one class for each choice: a tile type for the agent's cell
- * (as pcgrl_step takes it), or a cell and a tile type for a policy that chooses both.  A class may
+ * (as pcgrl_step takes it), or a cell and a tile type for a policy that chooses both (what such a class does to a level is up to the
+ * caller: pcgrl_step and pcgrl_step_logits take the first kind).  A class may
  * be chosen if its mask byte is not 0 (mask NULL: all) and its logit is not -infinity.  Logits, values
  * and other numbers that masked classes hold are not looked at. */
 #define PCGRL_MAX_CLASSES 32768

@@ -359,7 +359,7 @@ template <typename T, int TEAM, int PER> struct Row {
 };
 
 // Keeps the compiler from taking more than four classes of a thread through a loop at once, by having the sums over them
-// done: what more take in registers costs more than it hides (28 672 classes a row went through scratch memory).
+// done: what more take in registers costs more than it hides (28 672 classes a row went through scratch memory; no loss does now).
 template <typename V> __device__ __forceinline__ void done(V& v) { asm volatile("" : "+v"(v)); }
 template <typename... V> __device__ __forceinline__ void part_end(int j, V&... sums) {
   if (j % 4 == 3) {
@@ -579,7 +579,9 @@ __device__ __forceinline__ Cutoff cut_by_halves(const float (&x)[PER], const dou
 // reduction over lanes is a dozen instructions for each row, and none of these need any; it finds each class's place by
 // comparing all pairs.  Eight or sixteen lanes use DPP moves, and halve the range of keys for the cutoff, 16 or 32 sums.
 // Bound by a launch up to some 20 000 rows (16 384 rows of 7 classes in bfloat16 3.4 us), then by 64-bit instructions: 262 144 rows of
-// 7 4.3 us, 1 000 000 of 4 8.8 us (2.3 TB/s), 100 000 of 64 10.0, 4096 of 200 3.8, with top_p 12.8.
+// 7 4.2 us, with top_p or top_k 8.2, 1 000 000 of 4 8.2 us (2.4 TB/s), 100 000 of 64 9.2, 4096 of 200 3.6, with top_p 12.2.  Cutoffs of
+// 65 to 256 classes keep 20 to 76 bytes a thread in scratch memory, draws of 257 to 512 without one up to 32: a row there is 16 or 32 classes a
+// thread, with a weight of 64 bits each, in 128 registers; with twice as many half the rows would be there to hide each other's waits.
 template <typename T, int TEAM, int PER, int HOW> __global__ __launch_bounds__(256, PER >= 16 ? 4 : 1) void sample_few_kernel(SampleArgs a) {
   static_assert(TEAM <= 16 && HOW != kSampleBest, "");
   using R = Row<T, TEAM, PER>;
@@ -1116,8 +1118,9 @@ __device__ __forceinline__ bool draw_from_list(const Stretch<T, TEAM>& in, const
 // weights, and the draw goes through the wavefront that has it.  For top_p the same pass bins them, a second lists the bin
 // in which the share is reached and sums what is above it.  For a top_k it counts them, and lists what may be kept.
 // Bound by 64-bit instructions, 34 a class in one pass and 87 in the two for top_p (1024 rows of 28 672 in bfloat16, masked: floor of the bytes
-// 16.3 us, one pass 38, of which 26 are instructions, with top_p 90, of which 65 are), and by waits where rows are few: one row of
-// 16 384 in float32 with top_k 14.3 us, one of 28 672 with top_p 29.
+// 16.3 us, one pass 37, of which 26 are instructions, with top_p 92, of which 65 are, with a top_k of 50 66, with one of 1000, which is counted
+// and then binned, 138), and by waits where rows are few: one row of 16 384 in float32 with top_k 15 us, one of 28 672 with top_p 27.  Cutoffs
+// of 16-bit types in 256 and 512 threads keep 8 to 12 bytes a thread in scratch memory.
 template <typename T, int TEAM, int HOW> __global__ __launch_bounds__(team_block<TEAM>(), 4) void sample_many_kernel(SampleArgs a) {
   static_assert(TEAM >= 64 && HOW != kSampleBest, "");
   using S = Stretch<T, TEAM>;
@@ -1248,9 +1251,9 @@ constexpr double kWidest = 0x1p40;
 // computed in 64 bits, from the logits again.  Sums of rows go to a workgroup's partials, which a second launch joins, in
 // the same order always (atomics would not, and have to be cleared first); that launch is 4 us of each figure below.
 // Bound by instructions, about 45 a class and 110 a row, which for one lane a row are shared by 64 rows: 2 097 152 rows of
-// 7 in bfloat16 39 us (floor of the bytes 18.6), 300 000 of 50 46, 20 000 of 500 21, 1001 of 8505 in float16 23 (7.9), 1024 of 16 384, masked,
-// 32 (15.5), 500 of 28 672 in float32 36 (21.2).  Rows of a wavefront put together in LDS for full stores were not faster (31 to 32 us for the
-// gradients alone), nor were eight places for 7 classes (43.9).
+// 7 in bfloat16 35 us (floor of the bytes 18.6), 300 000 of 50 44, 20 000 of 500 20, 1001 of 8505 in float16 23 (7.9), 1024 of 16 384, masked,
+// 31.5 (15.5), 500 of 28 672 in float32 35.5 (21.2).  Rows of a wavefront put together in LDS for full stores were not faster (31 to 32 us for the
+// gradients alone), nor were eight places for 7 classes (43.9, when seven took 39).
 template <typename T, int TEAM, int PER> __global__ __launch_bounds__(team_block<TEAM>(), PER >= 16 || TEAM >= 64 ? 4 : 1) void loss_kernel(LossArgs a) {
   using R = Row<T, TEAM, PER>;
   using raw = typename T::raw;
@@ -1508,8 +1511,8 @@ template <bool ALL> __device__ __forceinline__ double join_steps(int envs_log2, 
 // joined from the last to the first they give every thread the advantage behind its steps.  Every input
 // is read once into registers, and the next steps are asked for before these are joined, which is worth a third to
 // a half (128 steps of 65 536 environments 41 -> 22 us, 10 000 of 800 71 -> 46).
-// Bound by memory for many environments: 32 steps of 262 144 with bfloat16 values, 126 MB, 21 us (6.0 TB/s of 5.4 that a large
-// copy reaches, as part of it stays in the last-level cache); by the latency of a load and a join, 2.5 us, and of a launch
+// Bound by memory for many environments: 32 steps of 262 144 with bfloat16 values, 126 MB, 22.5 us where its arrays stay the same from call to
+// call (5.6 TB/s; a large copy reaches 5.4, as none of it stays in the last-level cache); by the latency of a load and a join, 2.5 us, and of a launch
 // for few.  Four environments a thread with 16-byte loads were not faster (26.5 against 21.6 us), nor workgroups of 1024 threads
 // (2000 steps of 64 9.1 against 9.9, 64 steps of 64 5.4 against 3.5).
 template <typename T, int MODE> __global__ __launch_bounds__(kAdvantageThreads) void advantages_kernel(AdvantageArgs a) {
