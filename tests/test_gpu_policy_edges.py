@@ -354,3 +354,34 @@ def test_actions_to_the_last_bits_of_the_weights(env, V):
     want, _, room = policy_oracle.sample(wide64(x), None, u)
     sure = room > V * (2.**-weight_bits(V) + 2.**-50)   # (0.7 steps a weight; the plain statement's own sums)
     assert sure.mean() > .3 and np.array_equal(got[sure], want[sure])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", CLASSES)
+def test_rows_in_64_bits_in_place_and_apart(env, V, dtype):
+    """Rows whose gradients are computed from the logits once more: written over them, in rows that lie apart, with one mask for
+    all rows, beside ordinary and uncounted rows, more than the machine holds at once; the same from call to call."""
+    rng, t = np.random.default_rng(V), TYPES[dtype]
+    n, pad = {2: 400000, 7: 400001, 40: 50001, 100: 50001, 200: 20001, 500: 20001}.get(V, 5001 if V <= 2000 else 2600 if V <= 4000 else 1100 if V <= 6000 else 600 if V <= 12000 else 300), 3
+    g = torch.Generator(DEV).manual_seed(V)
+    store = torch.empty((n, V + pad), dtype=t, device=DEV).normal_(0, 1.5, generator=g)
+    x, mask = store[:, :V], (torch.rand((V,), generator=g, device=DEV) < .8).to(torch.uint8)
+    mask[V // 2] = 1
+    a = torch.randint(0, V, (n,), generator=g, device=DEV).int()
+    adv = torch.randn((n,), generator=g, device=DEV)
+    old = torch.where(torch.rand((n,), generator=g, device=DEV) < .1, -60., math.log(1 / V))      # (every tenth ratio beyond 2^40)
+    old[5::97], a[7::89] = math.nan, -1
+    for how in (dict(old_log_probs=old, scale=1.), dict(temperature=1e-22, scale=1e-22), dict(entropy_coef=1e20, scale=1.)):
+        want = env.pcgrl_policy_loss(x, a, adv, mask=mask, **how)["grad_logits"]
+        again = env.pcgrl_policy_loss(x, a, adv, mask=mask.expand(n, V).contiguous(), **how)["grad_logits"]
+        copy = store.clone()
+        got = env.pcgrl_policy_loss(copy[:, :V], a, adv, mask=mask, grad_logits=copy[:, :V], **how)["grad_logits"]
+        bits = lambda v: v.contiguous().view(torch.int32 if t == torch.float32 else torch.int16)  # noqa: E731
+        assert torch.equal(bits(got), bits(want)) and torch.equal(bits(again), bits(want)) and torch.equal(bits(copy[:, V:]), bits(store[:, V:]))
+        rows = [0, 1, 5, 7, n // 2, n - 2, n - 1]
+        counted = [r for r in rows if int(a[r]) >= 0 and int(mask[int(a[r])]) != 0]
+        at = lambda v: None if v is None else v[counted].cpu().numpy()  # noqa: E731
+        if counted:
+            plain = dict(temperature=how.get("temperature", 1.), scale=how["scale"], entropy_coef=how.get("entropy_coef", .01), old=at(how.get("old_log_probs")))
+            check_gradient(want[counted], *gradients(wide64(x[counted]), np.broadcast_to(mask.cpu().numpy(), (len(counted), V)), at(a), at(adv), **plain), t)
+        assert not bool((want[[r for r in rows if r not in counted]] != 0).any())
